@@ -85,7 +85,8 @@ typedef enum {
     MOC_OP_DECODE = 2,
     MOC_OP_SWIGLU_FWD = 3,
     MOC_OP_SWIGLU_BWD = 4,
-    MOC_OP_FWD_KEYED = 5       /* moc_ffn_fwd_keyed: the forward workspace plus one fp32 [T, F] key array */
+    MOC_OP_FWD_KEYED = 5,      /* moc_ffn_fwd_keyed: the forward workspace plus one fp32 [T, F] key array */
+    MOC_OP_BWD_ACT8 = 6        /* moc_ffn_bwd_act8, moc_ffn_bwd_experts_act8: the backward workspace plus x, restored */
 } moc_op;
 
 /* What the row Top-K ranks (ablation "Effect of top-K's position" and the remark after the proof
@@ -220,6 +221,87 @@ moc_status moc_topk_grouped_rows(int32_t T, int32_t F, int32_t a, int32_t b, con
  * profiling", RMSNorm item); h, out are [T,d] in dtype, gain is [d] in dtype. */
 moc_status moc_rmsnorm(int32_t T, int32_t d, int32_t dtype, const void* h, const void* gain,
                        float eps, void* out, void* hip_stream);
+
+/* Backward of moc_rmsnorm.  With n = h / sqrt(mean(h^2) + eps) and p = dy . gain, a row of dh is
+ * (p - n mean(p . n)) / sqrt(mean(h^2) + eps), plus dres's row if dres_or_null is not NULL (the gradient
+ * that reaches h past the norm, over the residual connection); dgain[d] is the sum of dy . n over the
+ * rows.  The statistics are computed again from h.  dh may be dy or dres.  Sums are fp32, in an order that
+ * depends on T and d only; every output is rounded once.  d <= 16384 (MOC_ERR_UNSUPPORTED).  ws holds
+ * moc_norm_bwd_workspace_bytes(T, d, dtype) bytes (0 if these are invalid). */
+moc_status moc_rmsnorm_bwd(int32_t T, int32_t d, int32_t dtype, const void* h, const void* gain, float eps,
+                           const void* dy, const void* dres_or_null, void* dh, void* dgain,
+                           void* ws, size_t ws_bytes, void* hip_stream);
+size_t moc_norm_bwd_workspace_bytes(int32_t T, int32_t d, int32_t dtype);
+
+/* Layer norm of each row, out = (h - mean(h)) / sqrt(variance(h) + eps) . gain + bias, for blocks that
+ * have it in RMSNorm's place; the variance is the mean of the squared differences from the mean.
+ * h, out are [T,d] in dtype, gain and bias [d] in dtype (no bias: NULL).  out may be h.  d <= 16384. */
+moc_status moc_layernorm(int32_t T, int32_t d, int32_t dtype, const void* h, const void* gain,
+                         const void* bias_or_null, float eps, void* out, void* hip_stream);
+
+/* Backward of moc_layernorm: with n the normalised row and p = dy . gain,
+ * dh = (p - mean(p) - n mean(p . n)) / sqrt(variance + eps) (+ dres), dgain and, unless dbias_or_null is
+ * NULL, dbias the sums of dy . n and of dy over the rows.  Everything else as moc_rmsnorm_bwd. */
+moc_status moc_layernorm_bwd(int32_t T, int32_t d, int32_t dtype, const void* h, const void* gain, float eps,
+                             const void* dy, const void* dres_or_null, void* dh, void* dgain, void* dbias_or_null,
+                             void* ws, size_t ws_bytes, void* hip_stream);
+
+/* The stored set of a layer in 8 bits: x [T,d], and gvals, uvals [T,K], as whole numbers q with one byte e for
+ * every 32 consecutive values of a row (the last of a row may be shorter); the Top-K mask as one bit a channel.  A value is
+ * q 2^(e - 133); e is the fp32 exponent field of the largest magnitude v among the 32, q = v 2^(133 - e) rounded to
+ * the nearest whole number (halves to even) and held to -127 .. 127.  Restored values are exact in both dtypes and
+ * off by at most 2^(e - 134), half a step, or a whole step where the bound of 127 holds.  e < 8 is stored as 0: the
+ * 32 values, below 2^-119, are zeros.  e = 255: an infinity or a NaN was among them, all 32 are NaN.  About
+ * d + 2 K + F / 8 bytes a token instead of the 2 d + 8 K of a bf16 layer. */
+typedef struct {
+    int8_t* xq;       /* [T, d] */
+    uint8_t* xe;      /* [T, ceil(d / 32)] */
+    uint32_t* sel;    /* [T, ceil(F / 32)], channel j in bit j % 32 of word j / 32 */
+    int8_t* gq;       /* [T, K] */
+    uint8_t* ge;      /* [T, ceil(K / 32)] */
+    int8_t* uq;       /* [T, K] */
+    uint8_t* ue;      /* [T, ceil(K / 32)] */
+} moc_act8_set;
+
+/* moc_act8_save packs x and the stored set that any of the forward entry points left (idx rows ascend strictly and
+ * lie in [0, F)); moc_act8_load restores them.  The set itself is HOST memory, its arrays are DEVICE memory as
+ * everywhere.  They need no workspace. */
+moc_status moc_act8_save(const moc_shape* shape, const void* x, const int32_t* idx, const void* gvals, const void* uvals,
+                         const moc_act8_set* set, void* hip_stream);
+moc_status moc_act8_load(const moc_shape* shape, const moc_act8_set* set, void* x, int32_t* idx, void* gvals, void* uvals,
+                         void* hip_stream);
+
+/* moc_ffn_bwd and moc_ffn_bwd_experts from an 8-bit set: the same gradients, bit for bit, as theirs from what
+ * moc_act8_load restores (for every F of theirs; the experts' limit on F does not hold here), without the restored
+ * set in memory but for x, which the workspace (MOC_OP_BWD_ACT8) has room for. */
+moc_status moc_ffn_bwd_act8(const moc_shape* shape, const moc_act8_set* set, const void* wg, const void* wu, const void* wd,
+                            const void* dy, void* dx, void* dwg, void* dwu, void* dwd,
+                            void* ws, size_t ws_bytes, void* hip_stream);
+moc_status moc_ffn_bwd_experts_act8(const moc_shape* shape, int32_t n_experts, const int32_t* expert_offsets,
+                                    const moc_act8_set* set, const void* wg, const void* wu, const void* wd, const void* dy,
+                                    void* dx, void* dwg, void* dwu, void* dwd, void* ws, size_t ws_bytes, void* hip_stream);
+
+/* Softmax router before the expert entry points.  logits [T,E] in dtype, 1 <= k <= E, E <= 256, k <= 16.  The
+ * slots of token t hold its k largest logits in descending order, ties to the lower expert, -0.0 equal to +0.0:
+ * ids[T,k], and weights[T,k] (fp32), the softmax of the row there, divided by their sum if renorm is not 0.  A logit of -inf
+ * is never chosen: slots that find nothing else hold -1 and weight 0.  A token whose byte in valid_or_null is 0
+ * (padding) has no slots, whatever its logits are.  counts[E] are the experts' slots; order[T*k] lists the
+ * slots, t*k + j, by expert and for each expert by token -- rows of x in this order and the running sum of counts are
+ * what moc_ffn_fwd_experts takes -- and -1 behind the last of them.  With A the sum of counts and N the
+ * tokens that have a slot, loss[1] = E sum_e (counts_e / A) (sum_t p_te / N), p the softmax of those tokens, and
+ * coef[E] = E counts_e / (A N), its derivative by any p_te (all zero if no token has a slot).  A NaN is never chosen either
+ * and makes the loss NaN.  The same inputs give the same bits.  T*k < 2^31 - 65536.  ws: moc_route_workspace_bytes. */
+size_t moc_route_workspace_bytes(int32_t T, int32_t E, int32_t k);
+moc_status moc_route(int32_t T, int32_t E, int32_t k, int32_t dtype, int32_t renorm, const void* logits,
+                     const uint8_t* valid_or_null, int32_t* ids, float* weights, int32_t* counts, int32_t* order,
+                     float* loss, float* coef, void* ws, size_t ws_bytes, void* hip_stream);
+
+/* Gradient of the router: dlogits[T,E] (dtype) from ids and coef of moc_route, dweights[T,k] (fp32) and dloss[1] (fp32);
+ * either may be NULL, for zero.  No gradient flows through the choice or the counts.  Rows of tokens without a slot
+ * are zero.  dweights of empty slots is not read into any result.  dlogits may be logits. */
+moc_status moc_route_bwd(int32_t T, int32_t E, int32_t k, int32_t dtype, int32_t renorm, const void* logits,
+                         const int32_t* ids, const float* coef, const float* dweights_or_null,
+                         const float* dloss_or_null, void* dlogits, void* hip_stream);
 
 /* Residual connection h <- h + y on [T,d] (same section, residual item). */
 moc_status moc_residual_add(int32_t T, int32_t d, int32_t dtype, void* h_inout, const void* y,

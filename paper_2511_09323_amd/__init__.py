@@ -10,4 +10,6 @@ from .binding import (  # noqa: F401
     moc_residual_add, moc_rmsnorm, moc_topk_grouped_rows,
     moc_swiglu_bwd, moc_swiglu_fwd, moc_topk_rows, timing_enable, timing_read, timing_reset, version,
     workspace_bytes,
+    Act8Set, OP_BWD_ACT8, Route, act8_empty, moc_act8_load, moc_act8_save, moc_ffn_bwd_act8, moc_ffn_bwd_experts_act8,
+    moc_layernorm, moc_layernorm_bwd, moc_rmsnorm_bwd, moc_route, moc_route_bwd, norm_bwd_workspace_bytes, route_workspace_bytes,
 )

@@ -9,6 +9,7 @@ the current torch stream through the C ABI declared in include/moc.h, and raises
 library returns a negative status.  There is no fallback: without the built library (or without a
 GPU tensor) the call fails.
 """
+import collections
 import ctypes
 import os
 
@@ -22,7 +23,9 @@ OP_FWD, OP_BWD, OP_DECODE, OP_SWIGLU_FWD, OP_SWIGLU_BWD = range(5)
 
 EXPORTS = (
     "moc_workspace_bytes", "moc_init", "moc_ffn_fwd", "moc_ffn_bwd", "moc_ffn_decode", "moc_ffn_decode_static", "moc_static_scratch_bytes", "moc_swiglu_fwd",
-    "moc_swiglu_bwd", "moc_topk_rows", "moc_ffn_fwd_experts", "moc_ffn_bwd_experts", "moc_ffn_fwd_keyed", "moc_ffn_decode_keyed", "moc_topk_rows_keyed", "moc_ffn_fwd_grouped", "moc_ffn_decode_grouped", "moc_topk_grouped_rows", "moc_rmsnorm", "moc_residual_add", "moc_timing_enable",
+    "moc_swiglu_bwd", "moc_topk_rows", "moc_ffn_fwd_experts", "moc_ffn_bwd_experts", "moc_ffn_fwd_keyed", "moc_ffn_decode_keyed", "moc_topk_rows_keyed", "moc_ffn_fwd_grouped", "moc_ffn_decode_grouped", "moc_topk_grouped_rows", "moc_rmsnorm", "moc_residual_add",
+    "moc_rmsnorm_bwd", "moc_layernorm", "moc_layernorm_bwd", "moc_norm_bwd_workspace_bytes", "moc_act8_save", "moc_act8_load", "moc_ffn_bwd_act8",
+    "moc_ffn_bwd_experts_act8", "moc_route", "moc_route_bwd", "moc_route_workspace_bytes", "moc_timing_enable",
     "moc_timing_collect", "moc_timing_get", "moc_timing_reset", "moc_status_string",
     "moc_last_error", "moc_version",
 )
@@ -37,6 +40,10 @@ class MocError(RuntimeError):
 class MocShape(ctypes.Structure):
     _fields_ = [("T", ctypes.c_int32), ("d", ctypes.c_int32), ("F", ctypes.c_int32),
                 ("K", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class MocAct8Set(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("xq", "xe", "sel", "gq", "ge", "uq", "ue")]
 
 
 _lib = None
@@ -104,6 +111,29 @@ def load_library():
     lib.moc_rmsnorm.argtypes = [i32, i32, i32, vp, vp, ctypes.c_float, vp, vp]
     lib.moc_residual_add.restype = ctypes.c_int
     lib.moc_residual_add.argtypes = [i32, i32, i32, vp, vp, vp]
+    act8 = ctypes.POINTER(MocAct8Set)
+    lib.moc_rmsnorm_bwd.restype = ctypes.c_int
+    lib.moc_rmsnorm_bwd.argtypes = [i32, i32, i32, vp, vp, ctypes.c_float, vp, vp, vp, vp, vp, sz, vp]
+    lib.moc_layernorm.restype = ctypes.c_int
+    lib.moc_layernorm.argtypes = [i32, i32, i32, vp, vp, vp, ctypes.c_float, vp, vp]
+    lib.moc_layernorm_bwd.restype = ctypes.c_int
+    lib.moc_layernorm_bwd.argtypes = [i32, i32, i32, vp, vp, ctypes.c_float, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.moc_norm_bwd_workspace_bytes.restype = sz
+    lib.moc_norm_bwd_workspace_bytes.argtypes = [i32, i32, i32]
+    lib.moc_act8_save.restype = ctypes.c_int
+    lib.moc_act8_save.argtypes = [shp, vp, vp, vp, vp, act8, vp]
+    lib.moc_act8_load.restype = ctypes.c_int
+    lib.moc_act8_load.argtypes = [shp, act8, vp, vp, vp, vp, vp]
+    lib.moc_ffn_bwd_act8.restype = ctypes.c_int
+    lib.moc_ffn_bwd_act8.argtypes = [shp, act8] + [vp] * 9 + [sz, vp]
+    lib.moc_ffn_bwd_experts_act8.restype = ctypes.c_int
+    lib.moc_ffn_bwd_experts_act8.argtypes = [shp, i32, ctypes.POINTER(i32), act8] + [vp] * 9 + [sz, vp]
+    lib.moc_route.restype = ctypes.c_int
+    lib.moc_route.argtypes = [i32, i32, i32, i32, i32] + [vp] * 9 + [sz, vp]
+    lib.moc_route_bwd.restype = ctypes.c_int
+    lib.moc_route_bwd.argtypes = [i32, i32, i32, i32, i32] + [vp] * 7
+    lib.moc_route_workspace_bytes.restype = sz
+    lib.moc_route_workspace_bytes.argtypes = [i32, i32, i32]
     lib.moc_timing_enable.restype = None
     lib.moc_timing_enable.argtypes = [ctypes.c_int]
     lib.moc_timing_collect.restype = i32
@@ -434,6 +464,7 @@ def moc_ffn_bwd_experts(x, offsets, wg, wu, wd, idx, gvals, uvals, dy, ws=None, 
 
 KEY_MODES = {"gate": 0, "silu": 1, "abs_silu": 2}
 OP_FWD_KEYED = 5
+OP_BWD_ACT8 = 6
 
 
 def _key_code(key):
@@ -606,6 +637,274 @@ def moc_residual_add(h, y):
     _check(lib.moc_residual_add(T, d, _dtype_code(h), _ptr(h, None, None, "h"), _ptr(y, h.dtype, (T, d), "y"),
                                 _stream()))
     return h
+
+
+# ------------------------------------------------- around the layer in training: norms, 8-bit stored sets, the router
+def _bad(text, *args):
+    return MocError("MOC_ERR_BAD_ARG", text % args)
+
+
+def _here(t, dtype, shape, name):
+    """_ptr for the entry points below, which also refuse a tensor that is not on the current device."""
+    p = _ptr(t, dtype, shape, name)
+    if t is not None and t.device.index != torch.cuda.current_device():
+        raise _bad("%s is on %s, the current device is %d", name, t.device, torch.cuda.current_device())
+    return p
+
+
+def _matrix(t, name):
+    if not isinstance(t, torch.Tensor) or t.dim() != 2:
+        raise _bad("%s must be a matrix", name)
+    return t.shape
+
+
+def _code(dtype):
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise _bad("unsupported torch dtype %s", dtype)
+    return MOC_F32 if dtype == torch.float32 else MOC_BF16
+
+
+def _scratch(ws, need, device):
+    """(workspace, its bytes); need = 0: the entry point finds the precise error."""
+    if ws is None:
+        ws = torch.empty(max(256, need), dtype=torch.uint8, device=device)
+    return ws, ws.numel() * ws.element_size()
+
+
+def norm_bwd_workspace_bytes(T, d, dtype):
+    return int(load_library().moc_norm_bwd_workspace_bytes(T, d, _code(dtype)))
+
+
+def route_workspace_bytes(T, E, k):
+    return int(load_library().moc_route_workspace_bytes(T, E, k))
+
+
+def moc_layernorm(h, gain, bias, eps, out=None):
+    """Layer norm of the rows of h [T,d]; gain, bias [d], bias may be None.  out may be h."""
+    if out is not None:
+        status = _fast.layernorm(h, gain, bias, eps, out)
+        if status != _NOT_TAKEN:
+            _check(status)
+            return out
+    lib = load_library()
+    T, d = _matrix(h, "h")
+    code = _code(h.dtype)
+    hp = _here(h, None, None, "h")
+    if out is None:
+        out = torch.empty_like(h)
+    _check(lib.moc_layernorm(T, d, code, hp, _here(gain, h.dtype, (d,), "gain"), _here(bias, h.dtype, (d,), "bias"), float(eps),
+                             _here(out, h.dtype, (T, d), "out"), _stream()))
+    return out
+
+
+def moc_layernorm_bwd(h, gain, eps, dy, dres=None, ws=None, out=None):
+    """Backward of moc_layernorm.  Returns (dh, dgain, dbias); dres, if given, is added to dh.  out: those three, dbias may be
+    None there, where the norm has no bias.  dh may be dy or dres."""
+    if out is not None and ws is not None:
+        dh, dgain, dbias = out
+        status = _fast.layernorm_bwd(h, gain, eps, dy, dres, dh, dgain, dbias, ws)
+        if status != _NOT_TAKEN:
+            _check(status)
+            return dh, dgain, dbias
+    lib = load_library()
+    T, d = _matrix(h, "h")
+    dt, code = h.dtype, _code(h.dtype)
+    hp = _here(h, None, None, "h")
+    if out is None:
+        out = torch.empty_like(h), torch.empty((d,), dtype=dt, device=h.device), torch.empty((d,), dtype=dt, device=h.device)
+    dh, dgain, dbias = out
+    ws, n = _scratch(ws, norm_bwd_workspace_bytes(T, d, dt), h.device)
+    _check(lib.moc_layernorm_bwd(T, d, code, hp, _here(gain, dt, (d,), "gain"), float(eps), _here(dy, dt, (T, d), "dy"), _here(dres, dt, (T, d), "dres"),
+                                 _here(dh, dt, (T, d), "dh"), _here(dgain, dt, (d,), "dgain"), _here(dbias, dt, (d,), "dbias"), _here(ws, None, None, "ws"), n,
+                                 _stream()))
+    return dh, dgain, dbias
+
+
+def moc_rmsnorm_bwd(h, gain, eps, dy, dres=None, ws=None, out=None):
+    """Backward of moc_rmsnorm.  Returns (dh, dgain); dres, if given, is added to dh.  dh may be dy or dres."""
+    if out is not None and ws is not None:
+        dh, dgain = out
+        status = _fast.rmsnorm_bwd(h, gain, eps, dy, dres, dh, dgain, ws)
+        if status != _NOT_TAKEN:
+            _check(status)
+            return dh, dgain
+    lib = load_library()
+    T, d = _matrix(h, "h")
+    dt, code = h.dtype, _code(h.dtype)
+    hp = _here(h, None, None, "h")
+    if out is None:
+        out = torch.empty_like(h), torch.empty((d,), dtype=dt, device=h.device)
+    dh, dgain = out
+    ws, n = _scratch(ws, norm_bwd_workspace_bytes(T, d, dt), h.device)
+    _check(lib.moc_rmsnorm_bwd(T, d, code, hp, _here(gain, dt, (d,), "gain"), float(eps), _here(dy, dt, (T, d), "dy"), _here(dres, dt, (T, d), "dres"),
+                               _here(dh, dt, (T, d), "dh"), _here(dgain, dt, (d,), "dgain"), _here(ws, None, None, "ws"), n, _stream()))
+    return dh, dgain
+
+
+Act8Set = collections.namedtuple("Act8Set", "xq xe sel gq ge uq ue")
+
+
+def _act8_shapes(T, d, F, K):
+    b = lambda n: (n + 31) // 32
+    return Act8Set((torch.int8, (T, d)), (torch.uint8, (T, b(d))), (torch.int32, (T, b(F))), (torch.int8, (T, K)), (torch.uint8, (T, b(K))),
+                   (torch.int8, (T, K)), (torch.uint8, (T, b(K))))
+
+
+def act8_empty(T, d, F, K, device="cuda"):
+    """The arrays of an 8-bit stored set (include/moc.h, moc_act8_set), not initialised: (xq, xe, sel, gq, ge, uq, ue)."""
+    return Act8Set(*(torch.empty(shape, dtype=dt, device=device) for dt, shape in _act8_shapes(T, d, F, K)))
+
+
+def _act8(saved, T, d, F, K):
+    if len(saved) != 7:
+        raise _bad("saved must hold xq, xe, sel, gq, ge, uq, ue")
+    want = _act8_shapes(T, d, F, K)
+    return MocAct8Set(*(_here(t, dt, shape, name).value if t is not None else None for name, t, (dt, shape) in zip(Act8Set._fields, saved, want)))
+
+
+def _act8_dims(saved):
+    """(T, d, K) by the set's arrays."""
+    T, d = _matrix(saved[0], "xq")
+    return T, d, _matrix(saved[3], "gq")[1]
+
+
+def moc_act8_save(x, idx, gvals, uvals, F, out=None):
+    """A layer's stored set in 8 bits: x [T,d] and idx, gvals, uvals [T,K] of a forward call over F channels.  Returns an Act8Set."""
+    if out is not None:
+        status = _fast.act8_save(x, idx, gvals, uvals, F, *out)
+        if status != _NOT_TAKEN:
+            _check(status)
+            return out
+    lib = load_library()
+    T, d = _matrix(x, "x")
+    K = _matrix(idx, "idx")[1]
+    dt = x.dtype
+    shp = _shape(T, d, F, K, _code(dt))
+    xp = _here(x, None, None, "x")
+    if out is None:
+        out = act8_empty(T, d, F, K, x.device)
+    _check(lib.moc_act8_save(ctypes.byref(shp), xp, _here(idx, torch.int32, (T, K), "idx"), _here(gvals, dt, (T, K), "gvals"), _here(uvals, dt, (T, K), "uvals"),
+                             ctypes.byref(_act8(out, T, d, F, K)), _stream()))
+    return out
+
+
+def moc_act8_load(saved, F, dtype, out=None):
+    """What an 8-bit stored set stands for: (x, idx, gvals, uvals) in dtype, as moc_ffn_bwd takes them."""
+    if out is not None:
+        status = _fast.act8_load(F, *saved, *out)
+        if status != _NOT_TAKEN:
+            _check(status)
+            return out
+    lib = load_library()
+    T, d, K = _act8_dims(saved)
+    shp = _shape(T, d, F, K, _code(dtype))
+    arr = _act8(saved, T, d, F, K)
+    if out is None:
+        dev = saved[0].device
+        out = (torch.empty((T, d), dtype=dtype, device=dev), torch.empty((T, K), dtype=torch.int32, device=dev),
+               torch.empty((T, K), dtype=dtype, device=dev), torch.empty((T, K), dtype=dtype, device=dev))
+    x, idx, gvals, uvals = out
+    _check(lib.moc_act8_load(ctypes.byref(shp), ctypes.byref(arr), _here(x, dtype, (T, d), "x"), _here(idx, torch.int32, (T, K), "idx"),
+                             _here(gvals, dtype, (T, K), "gvals"), _here(uvals, dtype, (T, K), "uvals"), _stream()))
+    return out
+
+
+def _bwd_act8(saved, offsets, wg, wu, wd, dy, ws, out):
+    lib = load_library()
+    T, d, K = _act8_dims(saved)
+    _matrix(dy, "dy")
+    dt, code = dy.dtype, _code(dy.dtype)
+    if not isinstance(wg, torch.Tensor) or wg.dim() != (2 if offsets is None else 3):
+        raise _bad("wg must be [F, d]" if offsets is None else "wg must be [n_experts, F, d]")
+    F = wg.shape[-2]
+    w = tuple(wg.shape[:-1]) + (d,)
+    dyp = _here(dy, dt, (T, d), "dy")
+    if out is None:
+        out = (torch.empty_like(dy),) + tuple(torch.empty(w, dtype=dt, device=dy.device) for _ in range(3))
+    dx, dwg, dwu, dwd = out
+    ws, n = _scratch(ws, workspace_bytes(T, d, F, K, dt, OP_BWD_ACT8), dy.device)
+    head = [ctypes.byref(_shape(T, d, F, K, code))]
+    if offsets is not None:
+        off, E = _offsets(offsets)
+        if E != w[0]:
+            raise _bad("offsets must have n_experts + 1 entries")
+        head += [E, off]
+    call = lib.moc_ffn_bwd_act8 if offsets is None else lib.moc_ffn_bwd_experts_act8
+    _check(call(*head, ctypes.byref(_act8(saved, T, d, F, K)), _here(wg, dt, w, "wg"), _here(wu, dt, w, "wu"), _here(wd, dt, w, "wd"), dyp,
+                _here(dx, dt, (T, d), "dx"), _here(dwg, dt, w, "dwg"), _here(dwu, dt, w, "dwu"), _here(dwd, dt, w, "dwd"), _here(ws, None, None, "ws"), n,
+                _stream()))
+    return dx, dwg, dwu, dwd
+
+
+def moc_ffn_bwd_act8(saved, wg, wu, wd, dy, ws=None, out=None):
+    """moc_ffn_bwd from an 8-bit stored set.  Returns (dx, dwg, dwu, dwd)."""
+    if out is not None and ws is not None:
+        status = _fast.bwd_act8(*saved, wg, wu, wd, dy, *out, ws)
+        if status != _NOT_TAKEN:
+            _check(status)
+            return tuple(out)
+    return _bwd_act8(saved, None, wg, wu, wd, dy, ws, out)
+
+
+def moc_ffn_bwd_experts_act8(saved, offsets, wg, wu, wd, dy, ws=None, out=None):
+    """moc_ffn_bwd_experts from an 8-bit stored set.  Returns (dx, dwg, dwu, dwd)."""
+    if out is not None and ws is not None:
+        status = _fast.bwd_experts_act8(offsets, *saved, wg, wu, wd, dy, *out, ws)
+        if status != _NOT_TAKEN:
+            _check(status)
+            return tuple(out)
+    return _bwd_act8(saved, offsets, wg, wu, wd, dy, ws, out)
+
+
+Route = collections.namedtuple("Route", "ids weights counts order loss coef")
+
+
+def moc_route(logits, k, valid=None, renorm=True, ws=None, out=None):
+    """Softmax router: the k experts of every row of logits [T,E], their weights, the experts' counts, the slots in expert order,
+    the balance loss and its derivative by a token's probabilities.  valid: uint8 [T], 0 for padding.  Returns a Route."""
+    if out is not None and ws is not None:
+        status = _fast.route(logits, k, valid, renorm, *out, ws)
+        if status != _NOT_TAKEN:
+            _check(status)
+            return out if isinstance(out, Route) else Route(*out)
+    lib = load_library()
+    T, E = _matrix(logits, "logits")
+    code = _code(logits.dtype)
+    lp = _here(logits, None, None, "logits")
+    if not isinstance(k, int) or not 1 <= k <= E:
+        raise _bad("k must satisfy 1 <= k <= E (got k=%s, E=%d)", k, E)
+    if out is None:
+        new = lambda dt, *shape: torch.empty(shape, dtype=dt, device=logits.device)
+        out = (new(torch.int32, T, k), new(torch.float32, T, k), new(torch.int32, E), new(torch.int32, T * k), new(torch.float32, 1), new(torch.float32, E))
+    if len(out) != 6:
+        raise _bad("out must hold ids, weights, counts, order, loss, coef")
+    ids, weights, counts, order, loss, coef = out
+    ws, n = _scratch(ws, route_workspace_bytes(T, E, k), logits.device)
+    _check(lib.moc_route(T, E, k, code, 1 if renorm else 0, lp, _here(valid, torch.uint8, (T,), "valid"), _here(ids, torch.int32, (T, k), "ids"),
+                         _here(weights, torch.float32, (T, k), "weights"), _here(counts, torch.int32, (E,), "counts"),
+                         _here(order, torch.int32, (T * k,), "order"), _here(loss, torch.float32, (1,), "loss"), _here(coef, torch.float32, (E,), "coef"),
+                         _here(ws, None, None, "ws"), n, _stream()))
+    return Route(*out)
+
+
+def moc_route_bwd(logits, ids, coef, dweights=None, dloss=None, renorm=True, out=None):
+    """Gradient of moc_route's weights (dweights [T,k] fp32) and balance loss (dloss [1] fp32): dlogits [T,E].  out may be logits."""
+    if out is not None:
+        status = _fast.route_bwd(logits, ids, coef, dweights, dloss, renorm, out)
+        if status != _NOT_TAKEN:
+            _check(status)
+            return out
+    lib = load_library()
+    T, E = _matrix(logits, "logits")
+    k = _matrix(ids, "ids")[1]
+    code = _code(logits.dtype)
+    lp = _here(logits, None, None, "logits")
+    if out is None:
+        out = torch.empty_like(logits)
+    _check(lib.moc_route_bwd(T, E, k, code, 1 if renorm else 0, lp, _here(ids, torch.int32, (T, k), "ids"), _here(coef, torch.float32, (E,), "coef"),
+                             _here(dweights, torch.float32, (T, k), "dweights"), _here(dloss, torch.float32, (1,), "dloss"),
+                             _here(out, logits.dtype, (T, E), "out"), _stream()))
+    return out
 
 
 def timing_enable(on):

@@ -1,6 +1,6 @@
 """Builds the HIP library in-tree: paper_2511_09323_amd/libmoc_ffn.so (gfx950 only), and the _marshal extension beside it.
 
-The entry points are spread over four translation units that are compiled side by side and
+The entry points are spread over several translation units that are compiled side by side and
 linked into one shared library.  _marshal is the host-only Python extension that hands torch tensors to
 that library (csrc/marshal.cpp); it is compiled against the installed torch's headers.
 """
@@ -18,7 +18,7 @@ LIB = os.path.join(HERE, "libmoc_ffn.so")
 # (named for the interpreter it was built for: another one does not find it, and says so)
 MARSHAL = os.path.join(HERE, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))
 HEADER = os.path.join(os.path.dirname(HERE), "include", "moc.h")
-SOURCES = ["moc_api.hip", "moc_fwd.hip", "moc_bwd.hip", "moc_decode.hip"]
+SOURCES = ["moc_api.hip", "moc_fwd.hip", "moc_bwd.hip", "moc_decode.hip", "moc_norm.hip", "moc_act8.hip", "moc_route.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
@@ -81,7 +81,7 @@ def build(verbose=True, only=None):
     # moc_api.hip holds the version string with the source hash, so it is compiled every time
     todo = [(s, o) for s, o in zip(SOURCES, objs) if only is None or s in only or s == "moc_api.hip" or not os.path.exists(o)]
     define = ['-DMOC_SOURCE_HASH="%s"' % source_hash()]
-    with ThreadPoolExecutor(max_workers=5) as pool:
+    with ThreadPoolExecutor(max_workers=8) as pool:
         jobs = [pool.submit(_run, [HIPCC] + FLAGS + define + ["-c", os.path.join(CSRC, s), "-o", o], verbose) for s, o in todo]
         if only is None or "marshal.cpp" in only or marshal_is_stale():
             jobs.append(pool.submit(build_marshal, verbose))

@@ -106,6 +106,7 @@ int device_cu_count();          // compute units of the current device (after en
 moc_status check_shape(const moc_shape* s, bool decode);
 moc_status check_group(int F, int K, int ga, int gb);
 moc_status check_key_mode(int32_t key_mode);
+moc_status check_act8_set(const moc_act8_set* set);
 moc_status check_offsets(const moc_shape* shape, int32_t n_experts, const int32_t* off);
 
 #define CHECK_PTR(p)                                                                   \
@@ -114,12 +115,13 @@ moc_status check_offsets(const moc_shape* shape, int32_t n_experts, const int32_
         if (!aligned16(p)) return fail(MOC_ERR_BAD_ARG, "%s is not 16-byte aligned", #p); \
     } while (0)
 
-#define CHECK_WS(op)                                                                                  \
+#define CHECK_WS_BYTES(need)                                                                          \
     do {                                                                                              \
         CHECK_PTR(ws);                                                                                \
-        size_t need_ = moc_workspace_bytes(shape, op);                                                \
+        const size_t need_ = (need);                                                                  \
         if (ws_bytes < need_) return fail(MOC_ERR_WORKSPACE, "workspace: %zu bytes given, %zu needed", ws_bytes, need_); \
     } while (0)
+#define CHECK_WS(op) CHECK_WS_BYTES(moc_workspace_bytes(shape, op))
 
 // ------------------------------------------------------------------- workspace layouts
 struct Dims {
@@ -218,6 +220,10 @@ template <class E> struct BwdWs {      // dense [T, ldF] operands (+ the bit mas
     }
 };
 
+// The backward from an 8-bit set: x restored behind the other scratch.
+template <class E> E* act8_x(void* ws, const BwdWs<E>& W) { return reinterpret_cast<E*>(static_cast<unsigned char*>(ws) + W.bytes); }
+template <class E> size_t bwd_act8_bytes(const Dims& D) { return BwdWs<E>(nullptr, D, false).bytes + round_up_sz((size_t)D.T * D.d * sizeof(E), 256); }
+
 constexpr int kDecodeFusedMaxP = 512;
 
 constexpr size_t kDecodeSyncBytes = 32 * 1024;
@@ -271,6 +277,7 @@ template <class E> size_t workspace_for(const Dims& D, int op) {
         case MOC_OP_SWIGLU_FWD: return FwdWs<E>(nullptr, D, true).bytes;
         case MOC_OP_SWIGLU_BWD: return BwdWs<E>(nullptr, D, true).bytes;
         case MOC_OP_FWD_KEYED: return FwdWs<E>(nullptr, D, false, true).bytes;
+        case MOC_OP_BWD_ACT8: return bwd_act8_bytes<E>(D);
     }
     return 0;
 }

@@ -147,6 +147,12 @@ moc_status check_key_mode(int32_t key_mode) {
     return MOC_OK;
 }
 
+moc_status check_act8_set(const moc_act8_set* set) {
+    if (!set) return fail(MOC_ERR_BAD_ARG, "set is NULL");
+    CHECK_PTR(set->xq); CHECK_PTR(set->xe); CHECK_PTR(set->sel); CHECK_PTR(set->gq); CHECK_PTR(set->ge); CHECK_PTR(set->uq); CHECK_PTR(set->ue);
+    return MOC_OK;
+}
+
 moc_status check_offsets(const moc_shape* shape, int32_t n_experts, const int32_t* off) {
     if (n_experts < 1 || n_experts > kMaxExperts) return fail(MOC_ERR_UNSUPPORTED, "n_experts must be 1..%d (got %d)", kMaxExperts, n_experts);
     if (!off) return fail(MOC_ERR_BAD_ARG, "expert_offsets is NULL");
@@ -165,7 +171,7 @@ extern "C" {
 
 size_t moc_workspace_bytes(const moc_shape* shape, int op) {
     if (check_shape(shape, op == MOC_OP_DECODE) != MOC_OK) return 0;
-    if (op < MOC_OP_FWD || op > MOC_OP_FWD_KEYED) return 0;
+    if (op < MOC_OP_FWD || op > MOC_OP_BWD_ACT8) return 0;
     Dims D(*shape);
     return shape->dtype == MOC_BF16 ? workspace_for<bf16_t>(D, op) : workspace_for<float>(D, op);
 }
