@@ -265,7 +265,7 @@ typedef struct {
 
 /* moc_act8_save packs x and the stored set that any of the forward entry points left (idx rows ascend strictly and
  * lie in [0, F)); moc_act8_load restores them.  The set itself is HOST memory, its arrays are DEVICE memory as
- * everywhere.  They need no workspace. */
+ * everywhere.  They need no workspace.  d <= 2^24. */
 moc_status moc_act8_save(const moc_shape* shape, const void* x, const int32_t* idx, const void* gvals, const void* uvals,
                          const moc_act8_set* set, void* hip_stream);
 moc_status moc_act8_load(const moc_shape* shape, const moc_act8_set* set, void* x, int32_t* idx, void* gvals, void* uvals,

@@ -44,99 +44,164 @@ __device__ __forceinline__ uint32_t half_max_u32(uint32_t v) {
     return r[0] > r[1] ? r[0] : r[1];
 }
 
-// One row of n values, by the 256 threads of a workgroup.  VEC: n is a multiple of 8, rows start on 16 bytes (q: on 8); a thread
-// packs 8 values and 4 threads a block.  Otherwise a thread packs one value and half a wavefront a block.
-template <class E, bool VEC> __device__ __forceinline__ void act8_pack_row(const E* __restrict__ v, int n, int8_t* __restrict__ q, uint8_t* __restrict__ e) {
-    if (VEC) {
-        for (int i = threadIdx.x * 8; i < act8_blocks(n) * kAct8Block; i += 256 * 8) {      // (whole blocks of 4 threads)
-            float f[8];
+// A row is packed and unpacked by the 256 threads of a workgroup, in two ways.  Pieces: 8 values a thread, 4 threads a block; rows are
+// whole pieces and start on 16 bytes (their q on 8).  Single values: a value a thread, half a wavefront a block.
+template <class E> struct Act8Piece {
+    static constexpr int R = 8 / Vec16<E>::N;
+    u32x4_t raw[R];
+    __device__ __forceinline__ void load(const E* v, bool in) {
 #pragma unroll
-            for (int p = 0; p < 8; p += Vec16<E>::N) {
-                const u32x4_t raw = i < n ? *reinterpret_cast<const u32x4_t*>(v + i + p) : u32x4_t{0, 0, 0, 0};
-                Vec16<E>::unpack(raw, f + p);
-            }
-            uint32_t m = 0;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) m = max(m, __float_as_uint(f[k]) & 0x7FFFFFFFu);
-            const uint32_t ex = act8_exponent(quad_max_u32(m));
-            const float scale = act8_scale(ex);
-            uint32_t w[2] = {0, 0};
-#pragma unroll
-            for (int k = 0; k < 8; ++k) w[k / 4] |= (uint32_t)(act8_round(f[k], scale, ex) & 0xFF) << (k % 4 * 8);
-            if (i < n) *reinterpret_cast<u32x2_t*>(q + i) = u32x2_t{w[0], w[1]};
-            if ((threadIdx.x & 3) == 0) e[i / kAct8Block] = (uint8_t)ex;
-        }
-    } else {
-        for (int i = threadIdx.x; i < act8_blocks(n) * kAct8Block; i += 256) {
-            const float f = i < n ? Elem<E>::load(v + i) : 0.0f;
-            const uint32_t ex = act8_exponent(half_max_u32(__float_as_uint(f) & 0x7FFFFFFFu));
-            const int r = act8_round(f, act8_scale(ex), ex);
-            if (i < n) q[i] = (int8_t)r;
-            if ((threadIdx.x & 31) == 0) e[i / kAct8Block] = (uint8_t)ex;
-        }
+        for (int p = 0; p < R; ++p) raw[p] = in ? reinterpret_cast<const u32x4_t*>(v)[p] : u32x4_t{0, 0, 0, 0};
     }
+    __device__ __forceinline__ u32x2_t pack(uint32_t& e) const {
+        float f[8];
+#pragma unroll
+        for (int p = 0; p < R; ++p) Vec16<E>::unpack(raw[p], f + p * Vec16<E>::N);
+        uint32_t m = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) m = max(m, __float_as_uint(f[k]) & 0x7FFFFFFFu);
+        e = act8_exponent(quad_max_u32(m));
+        const float scale = act8_scale(e);
+        uint32_t w[2] = {0, 0};
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w[k / 4] |= (uint32_t)(act8_round(f[k], scale, e) & 0xFF) << (k % 4 * 8);
+        return u32x2_t{w[0], w[1]};
+    }
+};
+template <class E> __device__ __forceinline__ void act8_unpack_piece(u32x2_t w, uint32_t e, E* v) {
+    const float step = act8_step(e);
+    float f[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) f[k] = (float)(int8_t)(w[k / 4] >> (k % 4 * 8)) * step;
+#pragma unroll
+    for (int p = 0; p < 8; p += Vec16<E>::N) *reinterpret_cast<u32x4_t*>(v + p) = Vec16<E>::pack(f + p);
 }
-template <class E, bool VEC> __device__ __forceinline__ void act8_unpack_row(const int8_t* __restrict__ q, const uint8_t* __restrict__ e, int n, E* __restrict__ v) {
-    if (VEC) {
-        for (int i = threadIdx.x * 8; i < n; i += 256 * 8) {
-            const u32x2_t w = *reinterpret_cast<const u32x2_t*>(q + i);
-            const float step = act8_step(e[i / kAct8Block]);
-            float f[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) f[k] = (float)(int8_t)(w[k / 4] >> (k % 4 * 8)) * step;
-#pragma unroll
-            for (int p = 0; p < 8; p += Vec16<E>::N) *reinterpret_cast<u32x4_t*>(v + i + p) = Vec16<E>::pack(f + p);
-        }
-    } else {
-        for (int i = threadIdx.x; i < n; i += 256) Elem<E>::store(v + i, (float)q[i] * act8_step(e[i / kAct8Block]));
-    }
+__device__ __forceinline__ int act8_pack_one(float f, uint32_t& e) {
+    e = act8_exponent(half_max_u32(__float_as_uint(f) & 0x7FFFFFFFu));
+    return act8_round(f, act8_scale(e), e);
 }
 
-// One workgroup per token: x, then the gate and up values, then the mask (words in LDS).  Entries of idx outside [0, F) are ignored.
+// One workgroup per token.  A step takes 2048 values of x (256, where rows are not whole pieces) and 1024 slots: everything it reads is
+// asked for before anything is worked on, so that a row of the usual sizes costs one trip to memory.  The mask is put together in LDS.
+// Entries of idx outside [0, F) are ignored.
+constexpr int kAct8Slots = 4;      // of a thread in a step
 template <class E, bool VEC>
 __global__ __launch_bounds__(256) void act8_save_kernel(const E* __restrict__ x, const int32_t* __restrict__ idx, const E* __restrict__ g, const E* __restrict__ u, int d, int F,
                                                         int K, moc_act8_set set) {
     extern __shared__ uint32_t act8_words[];
     const int64_t t = blockIdx.x;
-    const int words = act8_blocks(F), kb = act8_blocks(K);
-    for (int i = threadIdx.x; i < words; i += 256) act8_words[i] = 0;
-    act8_pack_row<E, VEC>(x + t * d, d, set.xq + t * d, set.xe + t * act8_blocks(d));
-    act8_pack_row<E, false>(g + t * K, K, set.gq + t * K, set.ge + t * kb);
-    act8_pack_row<E, false>(u + t * K, K, set.uq + t * K, set.ue + t * kb);
-    __syncthreads();
-    for (int s = threadIdx.x; s < K; s += 256) {
-        const int j = idx[t * K + s];
-        if (j >= 0 && j < F) atomicOr(&act8_words[j >> 5], 1u << (j & 31));
+    const int tid = threadIdx.x, words = act8_blocks(F), db = act8_blocks(d), kb = act8_blocks(K);
+    constexpr int XSTEP = VEC ? 2048 : 256, KSTEP = 256 * kAct8Slots;
+    const int xend = db * kAct8Block, kend = kb * kAct8Block;      // whole blocks: their lanes stay together
+    for (int i = tid; i < words; i += 256) act8_words[i] = 0;
+    for (int x0 = 0, k0 = 0; x0 < d || k0 < K; x0 += XSTEP, k0 += KSTEP) {
+        const int xi = x0 + tid * (VEC ? 8 : 1);
+        Act8Piece<E> piece;
+        float one = 0.0f, gv[kAct8Slots], uv[kAct8Slots];
+        int ch[kAct8Slots];
+        if (VEC) piece.load(x + t * d + xi, xi < d);
+        else if (xi < d) one = Elem<E>::load(x + t * d + xi);
+#pragma unroll
+        for (int q = 0; q < kAct8Slots; ++q) {
+            const int s = k0 + q * 256 + tid;
+            ch[q] = s < K ? idx[t * K + s] : -1;
+            gv[q] = s < K ? Elem<E>::load(g + t * K + s) : 0.0f;
+            uv[q] = s < K ? Elem<E>::load(u + t * K + s) : 0.0f;
+        }
+        if (x0 == 0) __syncthreads();      // (the words are zero)
+        if (xi < xend) {
+            uint32_t e;
+            if (VEC) {
+                const u32x2_t w = piece.pack(e);
+                if (xi < d) *reinterpret_cast<u32x2_t*>(set.xq + t * d + xi) = w;
+            } else {
+                const int w = act8_pack_one(one, e);
+                if (xi < d) set.xq[t * d + xi] = (int8_t)w;
+            }
+            if (xi % kAct8Block == 0) set.xe[t * db + xi / kAct8Block] = (uint8_t)e;
+        }
+#pragma unroll
+        for (int q = 0; q < kAct8Slots; ++q) {
+            const int s = k0 + q * 256 + tid;
+            if (s >= kend) continue;
+            if (ch[q] >= 0 && ch[q] < F) atomicOr(&act8_words[ch[q] >> 5], 1u << (ch[q] & 31));
+            uint32_t eg, eu;
+            const int wg = act8_pack_one(gv[q], eg), wu = act8_pack_one(uv[q], eu);
+            if (s < K) {
+                set.gq[t * K + s] = (int8_t)wg;
+                set.uq[t * K + s] = (int8_t)wu;
+            }
+            if (s % kAct8Block == 0) {
+                set.ge[t * kb + s / kAct8Block] = (uint8_t)eg;
+                set.ue[t * kb + s / kAct8Block] = (uint8_t)eu;
+            }
+        }
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < words; i += 256) set.sel[t * words + i] = act8_words[i];
+    for (int i = tid; i < words; i += 256) set.sel[t * words + i] = act8_words[i];
 }
 
-// The inverse.  Channels are written in the order of the set bits; a row with fewer than K bits (not one that was saved) leaves the rest of its
-// indices at -1, bits past the K-th are dropped.
+// x of a row from its 8 bits
+template <class E, bool VEC> __device__ __forceinline__ void act8_unpack_row(const int8_t* __restrict__ q, const uint8_t* __restrict__ e, int n, E* __restrict__ v) {
+    if (VEC) {
+        for (int i = threadIdx.x * 8; i < n; i += 256 * 8) act8_unpack_piece<E>(*reinterpret_cast<const u32x2_t*>(q + i), e[i / kAct8Block], v + i);
+    } else {
+        for (int i = threadIdx.x; i < n; i += 256) Elem<E>::store(v + i, (float)q[i] * act8_step(e[i / kAct8Block]));
+    }
+}
+
+// The inverse, with the same steps.  Channels are written in the order of the set bits; a row with fewer than K bits (not one that was saved) leaves the
+// rest of its indices at -1, bits past the K-th are dropped.
 template <class E, bool VEC>
 __global__ __launch_bounds__(256) void act8_load_kernel(moc_act8_set set, int d, int F, int K, E* __restrict__ x, int32_t* __restrict__ idx, E* __restrict__ g, E* __restrict__ u) {
-    __shared__ int sums[4];
+    __shared__ int sums[2][4];
     const int64_t t = blockIdx.x;
-    const int words = act8_blocks(F), kb = act8_blocks(K), wave = threadIdx.x >> 6;
-    act8_unpack_row<E, VEC>(set.xq + t * d, set.xe + t * act8_blocks(d), d, x + t * d);
-    act8_unpack_row<E, false>(set.gq + t * K, set.ge + t * kb, K, g + t * K);
-    act8_unpack_row<E, false>(set.uq + t * K, set.ue + t * kb, K, u + t * K);
-    int base = 0;
-    for (int w0 = 0; w0 < words; w0 += 256) {
-        const int w = w0 + threadIdx.x;
+    const int tid = threadIdx.x, words = act8_blocks(F), db = act8_blocks(d), kb = act8_blocks(K), wave = tid >> 6;
+    constexpr int XSTEP = VEC ? 2048 : 256, KSTEP = 256 * kAct8Slots;
+    int base = 0, turn = 0;
+    for (int x0 = 0, k0 = 0, w0 = 0; x0 < d || k0 < K || w0 < words; x0 += XSTEP, k0 += KSTEP, w0 += 256, turn ^= 1) {
+        const int xi = x0 + tid * (VEC ? 8 : 1), w = w0 + tid;
         uint32_t bits = w < words ? set.sel[t * words + w] : 0;
-        if (w == words - 1 && (F & 31)) bits &= (1u << (F & 31)) - 1;
-        const int mine = __popc(bits), upto = wave_inclusive_sum(mine);
-        if ((threadIdx.x & 63) == 63) sums[wave] = upto;
-        __syncthreads();
-        int at = base + upto - mine;
-        for (int i = 0; i < wave; ++i) at += sums[i];
-        base += sums[0] + sums[1] + sums[2] + sums[3];
-        for (; bits != 0 && at < K; bits &= bits - 1) idx[t * K + at++] = w * 32 + __ffs(bits) - 1;
-        __syncthreads();
+        u32x2_t xw{0, 0};
+        uint32_t xe = 0;
+        float one = 0.0f, gv[kAct8Slots], uv[kAct8Slots];
+        uint32_t ge[kAct8Slots], ue[kAct8Slots];
+        if (xi < d) {
+            if (VEC) xw = *reinterpret_cast<const u32x2_t*>(set.xq + t * d + xi);
+            else one = (float)set.xq[t * d + xi];
+            xe = set.xe[t * db + xi / kAct8Block];
+        }
+#pragma unroll
+        for (int q = 0; q < kAct8Slots; ++q) {
+            const int s = k0 + q * 256 + tid;
+            gv[q] = s < K ? (float)set.gq[t * K + s] : 0.0f;
+            uv[q] = s < K ? (float)set.uq[t * K + s] : 0.0f;
+            ge[q] = s < K ? set.ge[t * kb + s / kAct8Block] : 0u;
+            ue[q] = s < K ? set.ue[t * kb + s / kAct8Block] : 0u;
+        }
+        if (w0 < words) {
+            if (w == words - 1 && (F & 31)) bits &= (1u << (F & 31)) - 1;
+            const int mine = __popc(bits), upto = wave_inclusive_sum(mine);
+            if ((tid & 63) == 63) sums[turn][wave] = upto;
+            __syncthreads();
+            int at = base + upto - mine;
+            for (int i = 0; i < wave; ++i) at += sums[turn][i];
+            base += sums[turn][0] + sums[turn][1] + sums[turn][2] + sums[turn][3];
+            for (; bits != 0 && at < K; bits &= bits - 1) idx[t * K + at++] = w * 32 + __ffs(bits) - 1;
+        }
+        if (xi < d) {
+            if (VEC) act8_unpack_piece<E>(xw, xe, x + t * d + xi);
+            else Elem<E>::store(x + t * d + xi, one * act8_step(xe));
+        }
+#pragma unroll
+        for (int q = 0; q < kAct8Slots; ++q) {
+            const int s = k0 + q * 256 + tid;
+            if (s >= K) continue;
+            Elem<E>::store(g + t * K + s, gv[q] * act8_step(ge[q]));
+            Elem<E>::store(u + t * K + s, uv[q] * act8_step(ue[q]));
+        }
     }
-    for (int s = base + threadIdx.x; s < K; s += 256) idx[t * K + s] = -1;
+    for (int s = base + tid; s < K; s += 256) idx[t * K + s] = -1;
 }
 
 // The backward's pointwise step (bwd_expand_kernel) from the 8-bit set, and x restored beside it.  A wavefront takes kAct8Span channels of
@@ -146,9 +211,8 @@ constexpr int kAct8Span = 1024;
 template <class E>
 __global__ __launch_bounds__(256) void bwd_expand_act8_kernel(moc_act8_set set, const E* __restrict__ dzd, RowGroups groups, int rows, int T, int d, int F, int K, int64_t ldf,
                                                               int unpack_groups, E* __restrict__ x, E* __restrict__ zd, E* __restrict__ dgd, E* __restrict__ dud) {
-    constexpr int PER16 = 16 / sizeof(E);
+    constexpr int PER16 = 16 / sizeof(E), SLOTS = kAct8Span / 64, BATCH = 4;
     __shared__ __align__(16) E span[4][3][kAct8Span];
-    __shared__ uint16_t place[4][kAct8Span];
     if ((int)blockIdx.x < unpack_groups) {
         for (int64_t t = blockIdx.x; t < T; t += unpack_groups) {
             if (d % 8 == 0) act8_unpack_row<E, true>(set.xq + t * d, set.xe + t * act8_blocks(d), d, x + t * d);
@@ -165,37 +229,64 @@ __global__ __launch_bounds__(256) void bwd_expand_act8_kernel(moc_act8_set set, 
     const int width = (int)min((int64_t)kAct8Span, ldf - c0);       // a multiple of 8
     const int64_t t = row_token(groups, (int)row);
     u32x4_t* mine = reinterpret_cast<u32x4_t*>(span[wave][0]);
-    for (int i = lane; i < 3 * kAct8Span / PER16; i += 64) mine[i] = u32x4_t{0, 0, 0, 0};
+    const auto ordered = [] {      // (LDS keeps a wavefront's order; this keeps the compiler's)
+        __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    };
+    int channel[SLOTS], before = 0, n = 0;
     if (t >= 0) {
-        const int words = act8_blocks(F), kb = act8_blocks(K), w0 = c0 / 32;
+        const int words = act8_blocks(F), w0 = c0 / 32;
         const uint32_t* sel = set.sel + t * words;
-        int before = 0;
-        for (int w = lane; w < w0; w += 64) before += __popc(sel[w]);
         // half a word a lane
         const int w = w0 + lane / 2;
         uint32_t bits = w < words ? sel[w] : 0;
+        for (int v = lane; v < w0; v += 64) before += __popc(sel[v]);
         if (w == words - 1 && (F & 31)) bits &= (1u << (F & 31)) - 1;
         bits = lane & 1 ? bits >> 16 : bits & 0xFFFFu;
         const int own = __popc(bits), upto = wave_inclusive_sum(own);
         before = __builtin_amdgcn_readlane(wave_inclusive_sum(before), 63);
-        const int n = min(__builtin_amdgcn_readlane(upto, 63), K - before);      // (negative: the row has more bits than slots)
-        for (int at = upto - own; bits != 0; bits &= bits - 1) place[wave][at++] = (uint16_t)(lane * 16 + __ffs(bits) - 1);
-        __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");      // (LDS keeps a wavefront's order; this keeps the compiler's)
-        __builtin_amdgcn_wave_barrier();
-        for (int s = lane; s < n; s += 64) {
-            const int j = place[wave][s], k = before + s;
-            const float gv = (float)set.gq[t * K + k] * act8_step(set.ge[t * kb + k / kAct8Block]);
-            const float uv = (float)set.uq[t * K + k] * act8_step(set.ue[t * kb + k / kAct8Block]);
-            const float dz = Elem<E>::load(dzd + t * ldf + c0 + j);
+        n = min(__builtin_amdgcn_readlane(upto, 63), K - before);      // (negative: the row has more bits than slots)
+        // channels by place, through the LDS that the rows take next
+        uint16_t* place = reinterpret_cast<uint16_t*>(mine);
+        for (int at = upto - own; bits != 0; bits &= bits - 1) place[at++] = (uint16_t)(lane * 16 + __ffs(bits) - 1);
+        ordered();
+#pragma unroll
+        for (int q = 0; q < SLOTS; ++q) {
+            if (q * 64 >= n) break;
+            channel[q] = place[q * 64 + lane];
+        }
+        ordered();
+    }
+    for (int i = lane; i < 3 * kAct8Span / PER16; i += 64) mine[i] = u32x4_t{0, 0, 0, 0};
+    ordered();
+    const int kb = act8_blocks(K);
+#pragma unroll
+    for (int q0 = 0; q0 < SLOTS; q0 += BATCH) {      // (what BATCH slots read is asked for before any is worked on)
+        if (q0 * 64 >= n) break;
+        float gv[BATCH], uv[BATCH], dz[BATCH];
+        uint32_t ge[BATCH], ue[BATCH];
+#pragma unroll
+        for (int q = 0; q < BATCH; ++q) {
+            const int s = (q0 + q) * 64 + lane, k = before + s;
+            const bool in = s < n;
+            gv[q] = in ? (float)set.gq[t * K + k] : 0.0f;
+            uv[q] = in ? (float)set.uq[t * K + k] : 0.0f;
+            ge[q] = in ? set.ge[t * kb + k / kAct8Block] : 0u;
+            ue[q] = in ? set.ue[t * kb + k / kAct8Block] : 0u;
+            dz[q] = in ? Elem<E>::load(dzd + t * ldf + c0 + channel[q0 + q]) : 0.0f;
+        }
+#pragma unroll
+        for (int q = 0; q < BATCH; ++q) {
+            if ((q0 + q) * 64 + lane >= n) continue;
+            const int j = channel[q0 + q];
             float z, dg, du;
-            moc_bwd_pointwise(gv, uv, dz, z, dg, du);
+            moc_bwd_pointwise(gv[q] * act8_step(ge[q]), uv[q] * act8_step(ue[q]), dz[q], z, dg, du);
             Elem<E>::store(&span[wave][0][j], z);
             Elem<E>::store(&span[wave][1][j], dg);
             Elem<E>::store(&span[wave][2][j], du);
         }
-        __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
-        __builtin_amdgcn_wave_barrier();
     }
+    ordered();
     const int64_t at = row * ldf + c0;
     for (int i = lane; i < width / PER16; i += 64) {
         reinterpret_cast<u32x4_t*>(zd + at)[i] = mine[i];

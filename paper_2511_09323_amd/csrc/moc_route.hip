@@ -23,7 +23,10 @@ struct RouteWs {
     float* psum;
     size_t bytes;
     RouteWs(void* ws, int T, int E) {
-        chunk = std::max(256, (T + kRouteGroups - 1) / kRouteGroups);
+        // one pass of route_rows_kernel, 256 tokens at most, unless that makes too many workgroups
+        int lanes = 1;
+        while (lanes * kRoutePer < E) lanes *= 2;
+        chunk = std::max(route_threads(lanes) / lanes, (T + kRouteGroups - 1) / kRouteGroups);
         groups = (T + chunk - 1) / chunk;
         Carver c(ws);
         hist = c.take<int32_t>((size_t)groups * (E + 1));
@@ -45,13 +48,14 @@ template <class E> moc_status route(const E* logits, const RouteArgs& a, hipStre
     {
         Span span("route_rows", st);
         for_token<E>(a.E, [&](auto L, auto vec) {
-            hipLaunchKernelGGL((route_rows_kernel<E, L, vec>), dim3(a.groups), dim3(256), route_rows_lds(a.E), st, logits, a);
+            constexpr int threads = route_threads(L);
+            hipLaunchKernelGGL((route_rows_kernel<E, L, vec>), dim3(a.groups), dim3(threads), route_rows_words(a.E, threads) * 4, st, logits, a);
         });
     }
     HIP_TRY(hipGetLastError());
     if (a.groups == 1) return MOC_OK;
     Span span("route_order", st);
-    hipLaunchKernelGGL(route_order_kernel, dim3(a.groups), dim3(256), route_order_lds(a.E), st, a);
+    hipLaunchKernelGGL(route_order_kernel, dim3(a.groups + 1), dim3(256), route_words(a.E, 256) * 4, st, a);
     HIP_TRY(hipGetLastError());
     return MOC_OK;
 }

@@ -21,7 +21,7 @@ namespace moc {
 constexpr int kRoutePer = 8;              // logits of a lane
 constexpr int kMaxRouteExperts = 256;     // 32 lanes
 constexpr int kMaxRouteSlots = 16;
-constexpr int kRouteGroups = 256;         // most workgroups of a routing launch
+constexpr int kRouteGroups = 256;         // most workgroups of a routing launch (the places' histograms are read by all of them)
 
 // Reductions over the L lanes of a token (L = 1 .. 32, aligned), for all of them; every step's partner holds another part of them.
 template <int L, class T, class Op> __device__ __forceinline__ T token_reduce(T v, const Op& op) {
@@ -60,6 +60,17 @@ template <class E, bool VEC> __device__ __forceinline__ void route_logits(const 
     }
 }
 
+// Slots of a token are spread over its lanes: slot j is in lane j % L, register j / L.
+template <int L> constexpr int route_regs() { return L == 1 ? kRoutePer : (kMaxRouteSlots + L - 1) / L; }
+// f(register, lane of the token, slot) for the k slots in order; the register is a constant.
+template <int L, class F> __device__ __forceinline__ void route_slots(int k, const F& f) {
+#pragma unroll
+    for (int r = 0; r < route_regs<L>(); ++r) {
+        if (r * L >= k) break;
+        for (int l = 0; l < L && r * L + l < k; ++l) f(r, l, r * L + l);
+    }
+}
+
 struct RouteArgs {
     int T, E, k, chunk, groups;      // tokens of a workgroup, workgroups
     bool renorm;
@@ -68,106 +79,151 @@ struct RouteArgs {
     float* weights;
     int32_t *counts, *order;
     float *loss, *coef;
-    // by workgroup: copies of every expert, tokens with a slot, and the sum of p over the tokens
+    // by workgroup: copies of every expert, then tokens with a slot; and the sum of p over the tokens
     int32_t* hist;                   // [groups, E + 1]
     float* psum;                     // [groups, E]
 };
 
-// Places of a workgroup's copies, and the loss (workgroup 0).  `base` (LDS, E words) and `mask` (8 E words).
-__device__ __forceinline__ void route_order(const RouteArgs& a, int group, int* base, uint32_t* mask, int* total) {
+// A workgroup's 256 or more threads share out `groups` rows of values for E experts: thread tid takes expert tid % Ep of the rows part, part + parts, ...
+struct RouteShare {
+    int e, part, parts;
+    __device__ __forceinline__ RouteShare(int E) {
+        const int bits = 32 - __clz(E - 1 | 1);           // 2^bits >= E
+        e = threadIdx.x & ((1 << bits) - 1);
+        part = threadIdx.x >> bits;
+        parts = blockDim.x >> bits;
+    }
+};
+
+// The loss, its derivative and the counts.  `mem`: LDS, 2 * threads words of 8-byte alignment.
+__device__ __forceinline__ void route_loss(const RouteArgs& a, uint32_t* mem) {
     const int tid = threadIdx.x;
-    // copies of every expert in all workgroups, and in those before this one
-    for (int e = tid; e < a.E; e += 256) {
-        int all = 0, before = 0;
-        for (int g = 0; g < a.groups; ++g) {
-            const int n = a.hist[g * (a.E + 1) + e];
-            all += n;
-            before += g < group ? n : 0;
+    double* psum = reinterpret_cast<double*>(mem);
+    const RouteShare sh(a.E);
+    __shared__ int count[kMaxRouteExperts + 2];           // of every expert, tokens with a slot, all copies
+    for (int i = tid; i < a.E + 2; i += blockDim.x) count[i] = 0;
+    __syncthreads();
+    double p = 0.0;
+    if (sh.e < a.E) {
+        int n = 0;
+#pragma unroll 4
+        for (int g = sh.part; g < a.groups; g += sh.parts) {
+            n += a.hist[g * (a.E + 1) + sh.e];
+            p += (double)a.psum[g * a.E + sh.e];
         }
-        total[e] = all;
-        base[e] = before;
+        atomicAdd(&count[sh.e], n);
+        atomicAdd(&count[a.E + 1], n);
+    }
+    psum[tid] = p;
+    for (int g = tid; g < a.groups; g += blockDim.x) atomicAdd(&count[a.E], a.hist[g * (a.E + 1) + a.E]);
+    __syncthreads();
+    const int A = count[a.E + 1];
+    const double scale = A > 0 ? (double)a.E / ((double)A * (double)count[a.E]) : 0.0;
+    double term = 0.0;
+    if (tid < a.E) {
+        const int width = blockDim.x / sh.parts;
+        for (int q = 0; q < sh.parts; ++q) term += psum[q * width + tid];
+        term *= scale * count[tid];
+        if (A == 0) term = 0.0;
+        a.counts[tid] = count[tid];
+        a.coef[tid] = (float)(scale * count[tid]);
     }
     __syncthreads();
-    int A = 0;
-    for (int e = 0; e < a.E; ++e) A += total[e];
-    for (int e = tid; e < a.E; e += 256) {
-        int first = 0;
-        for (int f = 0; f < e; ++f) first += total[f];
-        base[e] += first;
-    }
-    if (group == 0) {
-        int N = 0;
-        for (int g = 0; g < a.groups; ++g) N += a.hist[g * (a.E + 1) + a.E];
-        const double scale = A > 0 ? (double)a.E / ((double)A * (double)N) : 0.0;
-        double* part = reinterpret_cast<double*>(mask);      // 8 E words hold E doubles
-        for (int e = tid; e < a.E; e += 256) {
-            double p = 0.0;
-            for (int g = 0; g < a.groups; ++g) p += (double)a.psum[g * a.E + e];
-            a.counts[e] = total[e];
-            a.coef[e] = (float)(scale * total[e]);
-            part[e] = A > 0 ? scale * total[e] * p : 0.0;
+    if (tid < a.E) psum[tid] = term;
+    __syncthreads();
+    if (tid >= 64) return;
+    term = 0.0;
+    for (int e = tid; e < a.E; e += 64) term += psum[e];
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) term += __shfl_xor(term, o, 64);
+    if (tid == 0) a.loss[0] = (float)term;
+}
+
+// The places of a workgroup's copies.  `mask`, `place`: LDS, 8 E words each.
+__device__ __forceinline__ void route_places(const RouteArgs& a, int group, uint32_t* mask, int* place) {
+    const int tid = threadIdx.x;
+    __shared__ int base[kMaxRouteExperts], all[kMaxRouteExperts], waves[4];
+    for (int i = tid; i < a.E; i += blockDim.x) base[i] = all[i] = 0;
+    __syncthreads();
+    // copies of every expert in all workgroups, and in those before this one
+    const RouteShare sh(a.E);
+    if (sh.e < a.E) {
+        int n = 0, before = 0;
+#pragma unroll 8
+        for (int g = sh.part; g < a.groups; g += sh.parts) {
+            const int h = a.hist[g * (a.E + 1) + sh.e];
+            n += h;
+            before += g < group ? h : 0;
         }
-        __syncthreads();
-        if (tid == 0) {
-            double s = 0.0;
-            for (int e = 0; e < a.E; ++e) s += part[e];
-            a.loss[0] = (float)s;
-        }
-        __syncthreads();
+        atomicAdd(&all[sh.e], n);
+        atomicAdd(&base[sh.e], before);
     }
+    __syncthreads();
+    int upto = 0, n = 0;
+    if (tid < 256) {
+        n = tid < a.E ? all[tid] : 0;
+        upto = wave_inclusive_sum(n);
+        if ((tid & 63) == 63) waves[tid >> 6] = upto;
+    }
+    __syncthreads();
+    if (tid < a.E) {
+        for (int w = 0; w < (tid >> 6); ++w) upto += waves[w];
+        base[tid] += upto - n;
+    }
+    const int A = waves[0] + waves[1] + waves[2] + waves[3];
     // 256 tokens at a time: a bit per token and expert gives every copy the number of those before it
     const int t1 = (int)min((int64_t)a.T, (int64_t)(group + 1) * a.chunk);
     for (int t0 = group * a.chunk; t0 < t1; t0 += 256) {
-        for (int i = tid; i < 8 * a.E; i += 256) mask[i] = 0;
+        for (int i = tid; i < 8 * a.E; i += blockDim.x) mask[i] = 0;
         __syncthreads();
-        const int t = t0 + tid;
-        if (t < t1)
-            for (int j = 0; j < a.k; ++j) {
-                const int e = a.ids[(int64_t)t * a.k + j];
-                if (e >= 0) atomicOr(&mask[e * 8 + (tid >> 5)], 1u << (tid & 31));
-            }
-        __syncthreads();
-        if (t < t1)
-            for (int j = 0; j < a.k; ++j) {
-                const int e = a.ids[(int64_t)t * a.k + j];
-                if (e < 0) continue;
-                int at = base[e] + __popc(mask[e * 8 + (tid >> 5)] & ((1u << (tid & 31)) - 1));
-                for (int w = 0; w < (tid >> 5); ++w) at += __popc(mask[e * 8 + w]);
-                a.order[at] = t * a.k + j;
-            }
-        __syncthreads();
-        for (int e = tid; e < a.E; e += 256) {
-            int n = 0;
-#pragma unroll
-            for (int w = 0; w < 8; ++w) n += __popc(mask[e * 8 + w]);
-            base[e] += n;
+        // (a copy a thread: its token's bit)
+        const int here = min(256, t1 - t0) * a.k;
+        const int32_t* ids = a.ids + (int64_t)t0 * a.k;
+        for (int c = tid; c < here; c += blockDim.x) {
+            const int e = ids[c], t = c / a.k;
+            if (e >= 0) atomicOr(&mask[e * 8 + (t >> 5)], 1u << (t & 31));
         }
         __syncthreads();
+        for (int i = tid; i < 8 * a.E; i += blockDim.x) {
+            const int e = i >> 3;
+            int at = base[e];
+            for (int w = e * 8; w < i; ++w) at += __popc(mask[w]);
+            place[i] = at;
+        }
+        __syncthreads();
+        for (int c = tid; c < here; c += blockDim.x) {
+            const int e = ids[c], t = c / a.k;
+            if (e >= 0) a.order[place[e * 8 + (t >> 5)] + __popc(mask[e * 8 + (t >> 5)] & ((1u << (t & 31)) - 1))] = t0 * a.k + c;
+        }
+        for (int e = tid; e < a.E; e += blockDim.x) base[e] = place[e * 8 + 7] + __popc(mask[e * 8 + 7]);
+        __syncthreads();
     }
-    for (int64_t i = (int64_t)A + group * 256 + tid; i < (int64_t)a.T * a.k; i += (int64_t)a.groups * 256) a.order[i] = -1;
+    for (int64_t i = (int64_t)A + group * blockDim.x + tid; i < (int64_t)a.T * a.k; i += (int64_t)a.groups * blockDim.x) a.order[i] = -1;
 }
 
-constexpr int route_order_lds(int E) { return (1 + 8 + 1) * E * 4; }
+// LDS of the places and the loss, words
+constexpr int route_words(int E, int threads) { return 16 * E > 2 * threads ? 16 * E : 2 * threads; }
 
+// The last workgroup is the loss's.
 static __global__ __launch_bounds__(256) void route_order_kernel(RouteArgs a) {
     extern __shared__ __align__(16) uint32_t route_smem[];
-    uint32_t* mask = route_smem;
-    int* base = reinterpret_cast<int*>(mask + 8 * a.E);
-    route_order(a, blockIdx.x, base, mask, base + a.E);
+    if ((int)blockIdx.x == a.groups) route_loss(a, route_smem);
+    else route_places(a, blockIdx.x, route_smem, reinterpret_cast<int*>(route_smem) + 8 * a.E);
 }
 
-// LDS: route_order's, and before that the sums of four wavefronts and the histogram (E + 1 words).
-constexpr int route_rows_lds(int E) {
-    const int rows = (4 * E + E + 1) * 4, order = route_order_lds(E);
+// LDS: of the places and the loss, and before that the wavefronts' sums and the histogram (E + 1 words).
+constexpr int route_threads(int L) { return L >= 4 ? 1024 : 256 * L; }
+constexpr int route_rows_words(int E, int threads) {
+    const int rows = (threads / 64) * E + E + 1, order = route_words(E, threads);
     return rows > order ? rows : order;
 }
-template <class E, int L, bool VEC> __global__ __launch_bounds__(256) void route_rows_kernel(const E* __restrict__ logits, RouteArgs a) {
+template <class E, int L, bool VEC> __global__ __launch_bounds__(route_threads(L)) void route_rows_kernel(const E* __restrict__ logits, RouteArgs a) {
     extern __shared__ __align__(16) uint32_t route_smem[];
-    float* sums = reinterpret_cast<float*>(route_smem);              // [4, E]
-    int* hist = reinterpret_cast<int*>(route_smem) + 4 * a.E;        // [E + 1]
-    constexpr int TOKENS = 256 / L;
+    constexpr int THREADS = route_threads(L), WAVES = THREADS / 64, TOKENS = THREADS / L, REGS = route_regs<L>();
+    float* sums = reinterpret_cast<float*>(route_smem);                  // [WAVES, E]
+    int* hist = reinterpret_cast<int*>(route_smem) + WAVES * a.E;        // [E + 1]
     const int lane = threadIdx.x % L, slot = threadIdx.x / L, e0 = lane * kRoutePer, wave = threadIdx.x >> 6;
-    for (int i = threadIdx.x; i <= a.E; i += 256) hist[i] = 0;
+    for (int i = threadIdx.x; i <= a.E; i += THREADS) hist[i] = 0;
     __syncthreads();
     float acc[kRoutePer];
 #pragma unroll
@@ -176,21 +232,17 @@ template <class E, int L, bool VEC> __global__ __launch_bounds__(256) void route
     for (int t0 = group * a.chunk; t0 < t1; t0 += TOKENS) {
         const int t = t0 + slot;
         if (t >= t1) continue;      // (a token's lanes leave together)
-        float l[kRoutePer];
+        float l[kRoutePer], ex[kRoutePer];
         route_logits<E, VEC>(logits + (int64_t)t * a.E, e0, a.E, l);
-        const bool in = !a.valid || a.valid[t] != 0;
+        bool used = !a.valid || a.valid[t] != 0;
         // keys: larger logits are larger, a NaN is below everything
         uint32_t key[kRoutePer];
 #pragma unroll
         for (int i = 0; i < kRoutePer; ++i) key[i] = l[i] == l[i] ? float_key(l[i]) : 0u;
         const uint32_t floor_key = float_key(-INFINITY);
-        float top = 0.0f, chosen = 0.0f;
-        int32_t* ids = a.ids + (int64_t)t * a.k;
-        float* weights = a.weights + (int64_t)t * a.k;
-        float ex[kRoutePer];
-        float all = 0.0f;
-        bool used = in;
-        for (int j = 0; j < a.k; ++j) {
+        float top = 0.0f, chosen = 0.0f, all = 1.0f, mine_x[REGS];
+        int mine_e[REGS];
+        route_slots<L>(a.k, [&](int r, int holder, int j) {
             uint32_t best = 0;
             int at = 0;
 #pragma unroll
@@ -204,30 +256,30 @@ template <class E, int L, bool VEC> __global__ __launch_bounds__(256) void route
                 top = key_float(row);
                 float s = 0.0f;
 #pragma unroll
-                for (int i = 0; i < kRoutePer; ++i) ex[i] = live ? (e0 + i < a.E ? expf(l[i] - top) : 0.0f) : 0.0f, s += ex[i];
+                for (int i = 0; i < kRoutePer; ++i) ex[i] = live && e0 + i < a.E ? expf(l[i] - top) : 0.0f, s += ex[i];
                 all = token_reduce<L>(s, OpSum());
-                if (live && lane == 0) atomicAdd(&hist[a.E], 1);
             }
             const float x = live ? expf(key_float(row) - top) : 0.0f;
             chosen += x;
-            if (lane == 0) {
-                ids[j] = live ? e : -1;
-                weights[j] = x;
-                if (live) atomicAdd(&hist[e], 1);
-            }
+            if (lane == holder) mine_e[r] = live ? e : -1, mine_x[r] = x;
 #pragma unroll
             for (int i = 0; i < kRoutePer; ++i)
                 if (e0 + i == e) key[i] = 0;
+        });
+        const float by = used ? (a.renorm ? chosen : all) : 1.0f, den = used ? 1.0f / all : 0.0f;
+#pragma unroll
+        for (int r = 0; r < REGS; ++r) {
+            const int j = r * L + lane;
+            if (j >= a.k) continue;
+            a.ids[(int64_t)t * a.k + j] = mine_e[r];
+            a.weights[(int64_t)t * a.k + j] = mine_x[r] / by;
+            if (mine_e[r] >= 0) atomicAdd(&hist[mine_e[r]], 1);
         }
-        const float den = used ? 1.0f / all : 0.0f;
-        if (lane == 0) {
-            const float by = a.renorm ? chosen : all;
-            for (int j = 0; j < a.k; ++j) weights[j] = used ? weights[j] / by : 0.0f;
-        }
+        if (used && lane == 0) atomicAdd(&hist[a.E], 1);
 #pragma unroll
         for (int i = 0; i < kRoutePer; ++i) acc[i] += ex[i] * den;
     }
-    // the wavefront's tokens, then its lanes in LDS
+    // the wavefront's tokens, then the wavefronts in LDS
 #pragma unroll
     for (int i = 0; i < kRoutePer; ++i) {
         float v = acc[i];
@@ -236,13 +288,18 @@ template <class E, int L, bool VEC> __global__ __launch_bounds__(256) void route
         if ((threadIdx.x & 63) < L && e0 + i < a.E) sums[wave * a.E + e0 + i] = v;
     }
     __syncthreads();
-    for (int e = threadIdx.x; e < a.E; e += 256) a.psum[group * a.E + e] = (sums[e] + sums[a.E + e]) + (sums[2 * a.E + e] + sums[3 * a.E + e]);
-    for (int e = threadIdx.x; e <= a.E; e += 256) a.hist[group * (a.E + 1) + e] = hist[e];
+    for (int e = threadIdx.x; e < a.E; e += THREADS) {
+        float v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) v += sums[w * a.E + e];
+        a.psum[group * a.E + e] = v;
+    }
+    for (int e = threadIdx.x; e <= a.E; e += THREADS) a.hist[group * (a.E + 1) + e] = hist[e];
     if (a.groups > 1) return;
     __syncthreads();      // the workgroup's own ids, sums and histogram are in memory; its LDS is free
-    uint32_t* mask = route_smem;
-    int* base = reinterpret_cast<int*>(mask + 8 * a.E);
-    route_order(a, 0, base, mask, base + a.E);
+    route_loss(a, route_smem);
+    __syncthreads();
+    route_places(a, 0, route_smem, reinterpret_cast<int*>(route_smem) + 8 * a.E);
 }
 
 // Gradient of the logits.  A token without a slot gets zeros, whatever its logits are.  dlogits may be logits: a lane writes what it alone read.
@@ -251,26 +308,34 @@ __global__ __launch_bounds__(256) void route_bwd_kernel(int T, int experts, int 
                                                         const float* __restrict__ coef, const float* __restrict__ dweights, const float* __restrict__ dloss,
                                                         E* dlogits) {
     const int64_t t = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
-    const int e0 = threadIdx.x % L * kRoutePer;
+    const int lane = threadIdx.x % L, e0 = lane * kRoutePer;
     if (t >= T) return;
     float out[kRoutePer];
 #pragma unroll
     for (int i = 0; i < kRoutePer; ++i) out[i] = 0.0f;
     if (ids[t * k] >= 0) {
-        float l[kRoutePer], ex[kRoutePer], dw[kRoutePer];
+        float l[kRoutePer], ex[kRoutePer], dw[kRoutePer], mine_w[route_regs<L>()];
+        int mine_e[route_regs<L>()];
         bool chosen[kRoutePer];
+#pragma unroll
+        for (int r = 0; r < route_regs<L>(); ++r) {
+            const int j = r * L + lane;
+            mine_e[r] = j < k ? ids[t * k + j] : -1;
+            mine_w[r] = j < k && dweights ? dweights[t * k + j] : 0.0f;
+        }
         route_logits<E, VEC>(logits + t * experts, e0, experts, l);
         float top = -INFINITY;
 #pragma unroll
         for (int i = 0; i < kRoutePer; ++i) top = fmaxf(top, l[i]), dw[i] = 0.0f, chosen[i] = false;
         top = token_reduce<L>(top, OpMax());
-        for (int j = 0; j < k; ++j) {
-            const int e = ids[t * k + j];
-            const float w = dweights ? dweights[t * k + j] : 0.0f;
+        route_slots<L>(k, [&](int r, int holder, int) {
+            const int from = (threadIdx.x & 63) - lane + holder;
+            const int e = L == 1 ? mine_e[r] : __shfl(mine_e[r], from, 64);
+            const float w = L == 1 ? mine_w[r] : __shfl(mine_w[r], from, 64);
 #pragma unroll
             for (int i = 0; i < kRoutePer; ++i)
                 if (e == e0 + i) dw[i] = w, chosen[i] = true;
-        }
+        });
         const float scale = dloss ? dloss[0] : 0.0f;
         float c[kRoutePer];
         float all = 0.0f, part = 0.0f, wdw = 0.0f, pc = 0.0f;
