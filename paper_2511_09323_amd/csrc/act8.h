@@ -220,11 +220,11 @@ __global__ __launch_bounds__(256) void bwd_expand_act8_kernel(moc_act8_set set, 
         }
         return;
     }
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int spans = (int)((ldf + kAct8Span - 1) / kAct8Span);
-    const int64_t task = (int64_t)(blockIdx.x - unpack_groups) * 4 + wave;
-    const int64_t row = task / spans;
-    if (row >= rows) return;
+    // (the wavefront's number is the same in all its lanes: what follows from it stays out of the vector registers)
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const unsigned spans = (unsigned)(ldf + kAct8Span - 1) / kAct8Span, task = (blockIdx.x - unpack_groups) * 4u + wave;      // (ldf < 2^16, tasks < 2^32)
+    const unsigned row = task / spans;
+    if (row >= (unsigned)rows) return;
     const int c0 = (int)(task - row * spans) * kAct8Span;
     const int width = (int)min((int64_t)kAct8Span, ldf - c0);       // a multiple of 8
     const int64_t t = row_token(groups, (int)row);
@@ -259,35 +259,38 @@ __global__ __launch_bounds__(256) void bwd_expand_act8_kernel(moc_act8_set set, 
     }
     for (int i = lane; i < 3 * kAct8Span / PER16; i += 64) mine[i] = u32x4_t{0, 0, 0, 0};
     ordered();
-    const int kb = act8_blocks(K);
+    const int8_t *gq = set.gq + t * K + before, *uq = set.uq + t * K + before;
+    const uint8_t *ge = set.ge + t * act8_blocks(K), *ue = set.ue + t * act8_blocks(K);
+    const E* dzrow = dzd + t * ldf + c0;
 #pragma unroll
     for (int q0 = 0; q0 < SLOTS; q0 += BATCH) {      // (what BATCH slots read is asked for before any is worked on)
         if (q0 * 64 >= n) break;
         float gv[BATCH], uv[BATCH], dz[BATCH];
-        uint32_t ge[BATCH], ue[BATCH];
+        uint32_t gx[BATCH], ux[BATCH];
 #pragma unroll
         for (int q = 0; q < BATCH; ++q) {
-            const int s = (q0 + q) * 64 + lane, k = before + s;
-            const bool in = s < n;
-            gv[q] = in ? (float)set.gq[t * K + k] : 0.0f;
-            uv[q] = in ? (float)set.uq[t * K + k] : 0.0f;
-            ge[q] = in ? set.ge[t * kb + k / kAct8Block] : 0u;
-            ue[q] = in ? set.ue[t * kb + k / kAct8Block] : 0u;
-            dz[q] = in ? Elem<E>::load(dzd + t * ldf + c0 + channel[q0 + q]) : 0.0f;
+            const int s = (q0 + q) * 64 + lane, block = (before + s) / kAct8Block;
+            if (s < n) {
+                gv[q] = (float)gq[s];
+                uv[q] = (float)uq[s];
+                gx[q] = ge[block];
+                ux[q] = ue[block];
+                dz[q] = Elem<E>::load(dzrow + channel[q0 + q]);
+            }
         }
 #pragma unroll
         for (int q = 0; q < BATCH; ++q) {
             if ((q0 + q) * 64 + lane >= n) continue;
             const int j = channel[q0 + q];
             float z, dg, du;
-            moc_bwd_pointwise(gv[q] * act8_step(ge[q]), uv[q] * act8_step(ue[q]), dz[q], z, dg, du);
+            moc_bwd_pointwise(gv[q] * act8_step(gx[q]), uv[q] * act8_step(ux[q]), dz[q], z, dg, du);
             Elem<E>::store(&span[wave][0][j], z);
             Elem<E>::store(&span[wave][1][j], dg);
             Elem<E>::store(&span[wave][2][j], du);
         }
     }
     ordered();
-    const int64_t at = row * ldf + c0;
+    const int64_t at = (int64_t)row * ldf + c0;
     for (int i = lane; i < width / PER16; i += 64) {
         reinterpret_cast<u32x4_t*>(zd + at)[i] = mine[i];
         reinterpret_cast<u32x4_t*>(dgd + at)[i] = mine[kAct8Span / PER16 + i];

@@ -49,13 +49,13 @@ template <class E> moc_status route(const E* logits, const RouteArgs& a, hipStre
         Span span("route_rows", st);
         for_token<E>(a.E, [&](auto L, auto vec) {
             constexpr int threads = route_threads(L);
-            hipLaunchKernelGGL((route_rows_kernel<E, L, vec>), dim3(a.groups), dim3(threads), route_rows_words(a.E, threads) * 4, st, logits, a);
+            hipLaunchKernelGGL((route_rows_kernel<E, L, vec>), dim3(a.groups), dim3(threads), route_rows_words(a.E, threads, a.groups == 1) * 4, st, logits, a);
         });
     }
     HIP_TRY(hipGetLastError());
     if (a.groups == 1) return MOC_OK;
     Span span("route_order", st);
-    hipLaunchKernelGGL(route_order_kernel, dim3(a.groups + 1), dim3(256), route_words(a.E, 256) * 4, st, a);
+    hipLaunchKernelGGL(route_order_kernel, dim3(a.groups + 1), dim3(kRouteOrderThreads), 0, st, a);
     HIP_TRY(hipGetLastError());
     return MOC_OK;
 }

@@ -86,21 +86,21 @@ __global__ __launch_bounds__(256) void layernorm_kernel(const E* h, const E* __r
     __shared__ float red[2][kMaxRowWaves];
     RowSums sums{red};
     const int lane = threadIdx.x % TPR;
-    const int64_t t = (int64_t)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
-    if (t >= T) return;                     // (whole rows: with TPR = 256 there is one a workgroup)
+    const int64_t t = (int64_t)blockIdx.x * (256 / TPR) + __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);      // (the same in a whole wavefront)
+    const int width = t < T ? d : 0;      // (rows past the last wait with the others)
     const E* x = h + t * d;
     typename Piece<E, W>::Raw raw[NV];
 #pragma unroll
     for (int u = 0; u < NV; ++u) {
         const int i = (u * TPR + lane) * W;
-        raw[u] = i < d ? Piece<E, W>::load(x + i) : Piece<E, W>::zero();
+        raw[u] = i < width ? Piece<E, W>::load(x + i) : Piece<E, W>::zero();
     }
     float mean, r;
     row_stats<E, W, NV, TPR, false>(raw, lane, d, eps, sums, mean, r);
 #pragma unroll
     for (int u = 0; u < NV; ++u) {
         const int i = (u * TPR + lane) * W;
-        if (i >= d) continue;
+        if (i >= width) continue;
         float v[W], g[W], b[W];
         Piece<E, W>::unpack(raw[u], v);
         Piece<E, W>::unpack(Piece<E, W>::load(gain + i), g);
@@ -121,7 +121,7 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(const E* __restrict__
     __shared__ float red[2][kMaxRowWaves];
     __shared__ float join[ROWS == 1 ? 1 : ROWS][ROWS == 1 ? 1 : TPR * W];
     RowSums sums{red};
-    const int lane = threadIdx.x % TPR, slot = threadIdx.x / TPR;
+    const int lane = threadIdx.x % TPR, slot = __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);      // (the same in a whole wavefront)
     const float scale = 1.0f / (float)d;
     float ag[NV * W], ab[BIAS ? NV * W : 1];
 #pragma unroll

@@ -84,139 +84,157 @@ struct RouteArgs {
     float* psum;                     // [groups, E]
 };
 
-// A workgroup's 256 or more threads share out `groups` rows of values for E experts: thread tid takes expert tid % Ep of the rows part, part + parts, ...
+// Threads share out `groups` rows of values for E experts: thread tid takes expert tid % width of the rows part, part + parts, ...
 struct RouteShare {
-    int e, part, parts;
+    int e, part, parts, width;
     __device__ __forceinline__ RouteShare(int E) {
-        const int bits = 32 - __clz(E - 1 | 1);           // 2^bits >= E
-        e = threadIdx.x & ((1 << bits) - 1);
+        const int bits = 32 - __clz((E - 1) | 1);           // 2^bits >= E
+        width = 1 << bits;
+        e = threadIdx.x & (width - 1);
         part = threadIdx.x >> bits;
         parts = blockDim.x >> bits;
     }
 };
 
-// The loss, its derivative and the counts.  `mem`: LDS, 2 * threads words of 8-byte alignment.
-__device__ __forceinline__ void route_loss(const RouteArgs& a, uint32_t* mem) {
+// The loss, its derivative and the counts, by the first wavefront, from every expert's copies, the tokens with a slot (count[E]) and the
+// sums of p: `parts` rows of `width` sums.
+template <class F> __device__ __forceinline__ void route_loss(const RouteArgs& a, const int* count, const F* psum, int parts, int width) {
     const int tid = threadIdx.x;
-    double* psum = reinterpret_cast<double*>(mem);
-    const RouteShare sh(a.E);
-    __shared__ int count[kMaxRouteExperts + 2];           // of every expert, tokens with a slot, all copies
-    for (int i = tid; i < a.E + 2; i += blockDim.x) count[i] = 0;
-    __syncthreads();
-    double p = 0.0;
-    if (sh.e < a.E) {
-        int n = 0;
-#pragma unroll 4
-        for (int g = sh.part; g < a.groups; g += sh.parts) {
-            n += a.hist[g * (a.E + 1) + sh.e];
-            p += (double)a.psum[g * a.E + sh.e];
-        }
-        atomicAdd(&count[sh.e], n);
-        atomicAdd(&count[a.E + 1], n);
-    }
-    psum[tid] = p;
-    for (int g = tid; g < a.groups; g += blockDim.x) atomicAdd(&count[a.E], a.hist[g * (a.E + 1) + a.E]);
-    __syncthreads();
-    const int A = count[a.E + 1];
-    const double scale = A > 0 ? (double)a.E / ((double)A * (double)count[a.E]) : 0.0;
-    double term = 0.0;
-    if (tid < a.E) {
-        const int width = blockDim.x / sh.parts;
-        for (int q = 0; q < sh.parts; ++q) term += psum[q * width + tid];
-        term *= scale * count[tid];
-        if (A == 0) term = 0.0;
-        a.counts[tid] = count[tid];
-        a.coef[tid] = (float)(scale * count[tid]);
-    }
-    __syncthreads();
-    if (tid < a.E) psum[tid] = term;
-    __syncthreads();
     if (tid >= 64) return;
-    term = 0.0;
-    for (int e = tid; e < a.E; e += 64) term += psum[e];
+    int A = 0;
+    for (int e = tid; e < a.E; e += 64) A += count[e];
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) term += __shfl_xor(term, o, 64);
-    if (tid == 0) a.loss[0] = (float)term;
+    for (int o = 32; o > 0; o >>= 1) A += __shfl_xor(A, o, 64);
+    const double scale = A > 0 ? (double)a.E / ((double)A * (double)count[a.E]) : 0.0;
+    double loss = 0.0;
+    for (int e = tid; e < a.E; e += 64) {
+        double p = 0.0;
+        for (int q = 0; q < parts; ++q) p += (double)psum[q * width + e];
+        if (A > 0) loss += scale * count[e] * p;
+        a.counts[e] = count[e];
+        a.coef[e] = (float)(scale * count[e]);
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) loss += __shfl_xor(loss, o, 64);
+    if (tid == 0) a.loss[0] = (float)loss;
 }
 
-// The places of a workgroup's copies.  `mask`, `place`: LDS, 8 E words each.
-__device__ __forceinline__ void route_places(const RouteArgs& a, int group, uint32_t* mask, int* place) {
+// The places of the copies of tokens t0 .. t0 + n - 1 (n <= 256), whose experts are in `ids` (of copy tid + THREADS * i): a bit per token and expert gives
+// every copy the number of those before it.  base[e] (LDS): the place of expert e's first one, moved on behind its last.  `mask`, `place`: LDS, 8 E words each;
+// mask is zero, and again after the call.
+constexpr int route_copies(int threads) { return 256 * kMaxRouteSlots / threads; }
+template <int THREADS> __device__ __forceinline__ void route_places(const RouteArgs& a, int t0, int n, const int* ids, int* base, uint32_t* mask, int* place) {
     const int tid = threadIdx.x;
-    __shared__ int base[kMaxRouteExperts], all[kMaxRouteExperts], waves[4];
-    for (int i = tid; i < a.E; i += blockDim.x) base[i] = all[i] = 0;
+#pragma unroll
+    for (int i = 0; i < route_copies(THREADS); ++i) {
+        const int c = tid + THREADS * i, t = c / a.k;
+        if (c < n * a.k && ids[i] >= 0) atomicOr(&mask[ids[i] * 8 + (t >> 5)], 1u << (t & 31));
+    }
     __syncthreads();
-    // copies of every expert in all workgroups, and in those before this one
+    for (int i = tid; i < 8 * a.E; i += THREADS) {
+        int at = base[i >> 3];
+        for (int w = i & ~7; w < i; ++w) at += __popc(mask[w]);
+        place[i] = at;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < route_copies(THREADS); ++i) {
+        const int c = tid + THREADS * i, t = c / a.k;
+        if (c >= n * a.k || ids[i] < 0) continue;
+        const int at = ids[i] * 8 + (t >> 5);
+        a.order[place[at] + __popc(mask[at] & ((1u << (t & 31)) - 1))] = t0 * a.k + c;
+    }
+    for (int e = tid; e < a.E; e += THREADS) base[e] = place[e * 8 + 7] + __popc(mask[e * 8 + 7]);
+    __syncthreads();
+    for (int i = tid; i < 8 * a.E; i += THREADS) mask[i] = 0;
+    __syncthreads();
+}
+template <int THREADS> __device__ __forceinline__ void route_ids(const RouteArgs& a, int t0, int n, int* ids) {
+#pragma unroll
+    for (int i = 0; i < route_copies(THREADS); ++i) {
+        const int c = threadIdx.x + THREADS * i;
+        ids[i] = c < n * a.k ? a.ids[(int64_t)t0 * a.k + c] : -1;
+    }
+}
+// base[e] += the copies of the experts before e, for up to 256 experts whose copies are in all[]; the result is their sum over all experts.  `waves`: LDS, 4 words.
+__device__ __forceinline__ int route_bases(int experts, const int* all, int* base, int* waves) {
+    const int tid = threadIdx.x;
+    int upto = 0, n = 0;
+    if (tid < 256) {
+        n = tid < experts ? all[tid] : 0;
+        upto = wave_inclusive_sum(n);
+        if ((tid & 63) == 63) waves[tid >> 6] = upto;
+    }
+    __syncthreads();
+    if (tid < experts) {
+        for (int w = 0; w < (tid >> 6); ++w) upto += waves[w];
+        base[tid] += upto - n;
+    }
+    __syncthreads();
+    return waves[0] + waves[1] + waves[2] + waves[3];
+}
+
+// Second launch.  A workgroup places its own copies; the last workgroup does the loss.
+constexpr int kRouteOrderThreads = 1024;
+static __global__ __launch_bounds__(kRouteOrderThreads) void route_order_kernel(RouteArgs a) {
+    constexpr int THREADS = kRouteOrderThreads;
+    __shared__ int all[kMaxRouteExperts + 1], base[kMaxRouteExperts], waves[4];
+    __shared__ __align__(16) uint32_t mem[2 * THREADS > 16 * kMaxRouteExperts ? 2 * THREADS : 16 * kMaxRouteExperts];
+    const int tid = threadIdx.x, group = blockIdx.x;
     const RouteShare sh(a.E);
+    if (group == a.groups) {
+        double* psum = reinterpret_cast<double*>(mem);
+        for (int i = tid; i <= a.E; i += THREADS) all[i] = 0;
+        __syncthreads();
+        double p = 0.0;
+        if (sh.e < a.E) {
+            int n = 0;
+#pragma unroll 4
+            for (int g = sh.part; g < a.groups; g += sh.parts) {
+                n += a.hist[g * (a.E + 1) + sh.e];
+                p += (double)a.psum[g * a.E + sh.e];
+            }
+            atomicAdd(&all[sh.e], n);
+        }
+        psum[tid] = p;
+        for (int g = tid; g < a.groups; g += THREADS) atomicAdd(&all[a.E], a.hist[g * (a.E + 1) + a.E]);
+        __syncthreads();
+        route_loss(a, all, psum, sh.parts, sh.width);
+        return;
+    }
+    const int t0 = group * a.chunk, t1 = (int)min((int64_t)a.T, (int64_t)t0 + a.chunk);
+    int ids[route_copies(THREADS)];
+    route_ids<THREADS>(a, t0, min(256, t1 - t0), ids);
+    // copies of every expert in all workgroups, and in those before this one
+    int n = 0, before = 0;
     if (sh.e < a.E) {
-        int n = 0, before = 0;
 #pragma unroll 8
         for (int g = sh.part; g < a.groups; g += sh.parts) {
             const int h = a.hist[g * (a.E + 1) + sh.e];
             n += h;
             before += g < group ? h : 0;
         }
+    }
+    for (int i = tid; i < a.E; i += THREADS) base[i] = all[i] = 0;
+    for (int i = tid; i < 8 * a.E; i += THREADS) mem[i] = 0;
+    __syncthreads();
+    if (sh.e < a.E) {
         atomicAdd(&all[sh.e], n);
         atomicAdd(&base[sh.e], before);
     }
     __syncthreads();
-    int upto = 0, n = 0;
-    if (tid < 256) {
-        n = tid < a.E ? all[tid] : 0;
-        upto = wave_inclusive_sum(n);
-        if ((tid & 63) == 63) waves[tid >> 6] = upto;
+    const int A = route_bases(a.E, all, base, waves);
+    for (int t = t0; t < t1; t += 256) {
+        if (t > t0) route_ids<THREADS>(a, t, min(256, t1 - t), ids);
+        route_places<THREADS>(a, t, min(256, t1 - t), ids, base, mem, reinterpret_cast<int*>(mem) + 8 * a.E);
     }
-    __syncthreads();
-    if (tid < a.E) {
-        for (int w = 0; w < (tid >> 6); ++w) upto += waves[w];
-        base[tid] += upto - n;
-    }
-    const int A = waves[0] + waves[1] + waves[2] + waves[3];
-    // 256 tokens at a time: a bit per token and expert gives every copy the number of those before it
-    const int t1 = (int)min((int64_t)a.T, (int64_t)(group + 1) * a.chunk);
-    for (int t0 = group * a.chunk; t0 < t1; t0 += 256) {
-        for (int i = tid; i < 8 * a.E; i += blockDim.x) mask[i] = 0;
-        __syncthreads();
-        // (a copy a thread: its token's bit)
-        const int here = min(256, t1 - t0) * a.k;
-        const int32_t* ids = a.ids + (int64_t)t0 * a.k;
-        for (int c = tid; c < here; c += blockDim.x) {
-            const int e = ids[c], t = c / a.k;
-            if (e >= 0) atomicOr(&mask[e * 8 + (t >> 5)], 1u << (t & 31));
-        }
-        __syncthreads();
-        for (int i = tid; i < 8 * a.E; i += blockDim.x) {
-            const int e = i >> 3;
-            int at = base[e];
-            for (int w = e * 8; w < i; ++w) at += __popc(mask[w]);
-            place[i] = at;
-        }
-        __syncthreads();
-        for (int c = tid; c < here; c += blockDim.x) {
-            const int e = ids[c], t = c / a.k;
-            if (e >= 0) a.order[place[e * 8 + (t >> 5)] + __popc(mask[e * 8 + (t >> 5)] & ((1u << (t & 31)) - 1))] = t0 * a.k + c;
-        }
-        for (int e = tid; e < a.E; e += blockDim.x) base[e] = place[e * 8 + 7] + __popc(mask[e * 8 + 7]);
-        __syncthreads();
-    }
-    for (int64_t i = (int64_t)A + group * blockDim.x + tid; i < (int64_t)a.T * a.k; i += (int64_t)a.groups * blockDim.x) a.order[i] = -1;
+    for (int64_t i = (int64_t)A + group * THREADS + tid; i < (int64_t)a.T * a.k; i += (int64_t)a.groups * THREADS) a.order[i] = -1;
 }
 
-// LDS of the places and the loss, words
-constexpr int route_words(int E, int threads) { return 16 * E > 2 * threads ? 16 * E : 2 * threads; }
-
-// The last workgroup is the loss's.
-static __global__ __launch_bounds__(256) void route_order_kernel(RouteArgs a) {
-    extern __shared__ __align__(16) uint32_t route_smem[];
-    if ((int)blockIdx.x == a.groups) route_loss(a, route_smem);
-    else route_places(a, blockIdx.x, route_smem, reinterpret_cast<int*>(route_smem) + 8 * a.E);
-}
-
-// LDS: of the places and the loss, and before that the wavefronts' sums and the histogram (E + 1 words).
+// First launch, and the only one where a workgroup holds all tokens (a.groups = 1).  LDS: the wavefronts' sums of p, the histogram (E + 1 words), and for a single
+// workgroup the places.
 constexpr int route_threads(int L) { return L >= 4 ? 1024 : 256 * L; }
-constexpr int route_rows_words(int E, int threads) {
-    const int rows = (threads / 64) * E + E + 1, order = route_words(E, threads);
-    return rows > order ? rows : order;
-}
+constexpr int route_rows_words(int E, int threads, bool one) { return (threads / 64) * E + E + 1 + (one ? 17 * E + 4 : 0); }
 template <class E, int L, bool VEC> __global__ __launch_bounds__(route_threads(L)) void route_rows_kernel(const E* __restrict__ logits, RouteArgs a) {
     extern __shared__ __align__(16) uint32_t route_smem[];
     constexpr int THREADS = route_threads(L), WAVES = THREADS / 64, TOKENS = THREADS / L, REGS = route_regs<L>();
@@ -287,6 +305,20 @@ template <class E, int L, bool VEC> __global__ __launch_bounds__(route_threads(L
         for (int o = L; o < 64; o <<= 1) v += __shfl_xor(v, o, 64);
         if ((threadIdx.x & 63) < L && e0 + i < a.E) sums[wave * a.E + e0 + i] = v;
     }
+    if (a.groups == 1) {
+        uint32_t* mask = route_smem + WAVES * a.E + a.E + 1;
+        int *place = reinterpret_cast<int*>(mask) + 8 * a.E, *base = place + 8 * a.E, *waves = base + a.E;
+        for (int i = threadIdx.x; i < 8 * a.E; i += THREADS) mask[i] = 0;
+        for (int i = threadIdx.x; i < a.E; i += THREADS) base[i] = 0;
+        __syncthreads();      // (the workgroup's own ids are in memory, too)
+        route_loss(a, hist, sums, WAVES, a.E);
+        int ids[route_copies(THREADS)];
+        route_ids<THREADS>(a, 0, a.T, ids);
+        const int A = route_bases(a.E, hist, base, waves);
+        route_places<THREADS>(a, 0, a.T, ids, base, mask, place);
+        for (int i = A + threadIdx.x; i < a.T * a.k; i += THREADS) a.order[i] = -1;
+        return;
+    }
     __syncthreads();
     for (int e = threadIdx.x; e < a.E; e += THREADS) {
         float v = 0.0f;
@@ -295,11 +327,6 @@ template <class E, int L, bool VEC> __global__ __launch_bounds__(route_threads(L
         a.psum[group * a.E + e] = v;
     }
     for (int e = threadIdx.x; e <= a.E; e += THREADS) a.hist[group * (a.E + 1) + e] = hist[e];
-    if (a.groups > 1) return;
-    __syncthreads();      // the workgroup's own ids, sums and histogram are in memory; its LDS is free
-    route_loss(a, route_smem);
-    __syncthreads();
-    route_places(a, 0, route_smem, reinterpret_cast<int*>(route_smem) + 8 * a.E);
 }
 
 // Gradient of the logits.  A token without a slot gets zeros, whatever its logits are.  dlogits may be logits: a lane writes what it alone read.
