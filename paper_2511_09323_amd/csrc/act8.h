@@ -23,183 +23,230 @@ __device__ __forceinline__ uint32_t act8_exponent(uint32_t amax_bits) {
 }
 // What values are multiplied with before rounding: 2^(133 - e), 0 where the block is zeros or NaN.
 __device__ __forceinline__ float act8_scale(uint32_t e) { return e == 0 || e == 255 ? 0.0f : __uint_as_float((260u - e) << 23); }
-__device__ __forceinline__ int act8_round(float v, float scale, uint32_t e) {
-    const int q = cvt_i32(fminf(fmaxf(rintf(v * scale), -127.0f), 127.0f));
-    return e == 255 ? 0 : q;
-}
 // What q is multiplied with: 2^(e - 133), 0, or NaN.  (e >= 8, so the power is 2^-125 at least.)
 __device__ __forceinline__ float act8_step(uint32_t e) {
     return e == 255 ? __uint_as_float(0x7FC00000u) : e < 8 ? 0.0f : __uint_as_float((e - 6u) << 23);
 }
 
+// Largest of 4 neighbouring lanes
 template <int CTRL> __device__ __forceinline__ uint32_t dpp_max_u32(uint32_t v) {
     const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, CTRL, 0xF, 0xF, false);
     return o > v ? o : v;
 }
-// Largest of 4 neighbouring lanes; of the 32 lanes of a half wavefront.
 __device__ __forceinline__ uint32_t quad_max_u32(uint32_t v) { return dpp_max_u32<0x4E>(dpp_max_u32<0xB1>(v)); }      // quad_perm [1,0,3,2], [2,3,0,1]
-__device__ __forceinline__ uint32_t half_max_u32(uint32_t v) {
-    v = dpp_max_u32<0x121>(dpp_max_u32<0x122>(dpp_max_u32<0x124>(dpp_max_u32<0x128>(v))));      // row_ror 8, 4, 2, 1
-    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
-    return r[0] > r[1] ? r[0] : r[1];
-}
 
-// A row is packed and unpacked by the 256 threads of a workgroup, in two ways.  Pieces: 8 values a thread, 4 threads a block; rows are
-// whole pieces and start on 16 bytes (their q on 8).  Single values: a value a thread, half a wavefront a block.
-template <class E> struct Act8Piece {
-    static constexpr int R = 8 / Vec16<E>::N;
-    u32x4_t raw[R];
-    __device__ __forceinline__ void load(const E* v, bool in) {
-#pragma unroll
-        for (int p = 0; p < R; ++p) raw[p] = in ? reinterpret_cast<const u32x4_t*>(v)[p] : u32x4_t{0, 0, 0, 0};
-    }
-    __device__ __forceinline__ u32x2_t pack(uint32_t& e) const {
-        float f[8];
-#pragma unroll
-        for (int p = 0; p < R; ++p) Vec16<E>::unpack(raw[p], f + p * Vec16<E>::N);
+// Rows are worked on in pieces of 8 values, 4 lanes a block.  Rows of K values start anywhere: pieces are loaded and stored at the element's alignment
+// (which the memory pipeline takes), the last ones of a row value by value.
+template <class E> struct Act8Piece;
+template <> struct Act8Piece<float> {
+    uint32_t raw[8];
+    __device__ __forceinline__ uint32_t top() const {      // bits of the largest magnitude
         uint32_t m = 0;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) m = max(m, __float_as_uint(f[k]) & 0x7FFFFFFFu);
-        e = act8_exponent(quad_max_u32(m));
-        const float scale = act8_scale(e);
-        uint32_t w[2] = {0, 0};
+        for (int k = 0; k < 8; ++k) m = max(m, raw[k] & 0x7FFFFFFFu);
+        return m;
+    }
+    __device__ __forceinline__ float value(int k) const { return __uint_as_float(raw[k]); }
+    __device__ __forceinline__ void set(int k, float v) { raw[k] = __float_as_uint(v); }
+};
+template <> struct Act8Piece<bf16_t> {
+    uint32_t raw[4];
+    typedef uint16_t Pair __attribute__((ext_vector_type(2)));
+    __device__ __forceinline__ uint32_t top() const {
+        Pair m = {0, 0};
 #pragma unroll
-        for (int k = 0; k < 8; ++k) w[k / 4] |= (uint32_t)(act8_round(f[k], scale, e) & 0xFF) << (k % 4 * 8);
-        return u32x2_t{w[0], w[1]};
+        for (int k = 0; k < 4; ++k) m = __builtin_elementwise_max(m, __builtin_bit_cast(Pair, raw[k] & 0x7FFF7FFFu));
+        const uint32_t lo = m.x, hi = m.y;
+        return (lo > hi ? lo : hi) << 16;
+    }
+    __device__ __forceinline__ float value(int k) const { return __uint_as_float(k & 1 ? raw[k / 2] & 0xFFFF0000u : raw[k / 2] << 16); }
+    __device__ __forceinline__ void set(int k, float v) {      // (in pairs; v has bf16's bits)
+        const uint32_t b = __float_as_uint(v);
+        raw[k / 2] = k & 1 ? (raw[k / 2] & 0xFFFFu) | (b & 0xFFFF0000u) : b >> 16;
     }
 };
-template <class E> __device__ __forceinline__ void act8_unpack_piece(u32x2_t w, uint32_t e, E* v) {
-    const float step = act8_step(e);
-    float f[8];
+template <class E> __device__ __forceinline__ void act8_read(Act8Piece<E>& p, const E* v, int left) {
+    if (left >= 8) {
+        __builtin_memcpy(p.raw, v, sizeof(p.raw));
+    } else {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) f[k] = (float)(int8_t)(w[k / 4] >> (k % 4 * 8)) * step;
+        for (int k = 0; k < 8; ++k) p.set(k, 0.0f);
 #pragma unroll
-    for (int p = 0; p < 8; p += Vec16<E>::N) *reinterpret_cast<u32x4_t*>(v + p) = Vec16<E>::pack(f + p);
+        for (int k = 0; k < 7; ++k)
+            if (k < left) p.set(k, Elem<E>::load(v + k));
+    }
 }
-__device__ __forceinline__ int act8_pack_one(float f, uint32_t& e) {
-    e = act8_exponent(half_max_u32(__float_as_uint(f) & 0x7FFFFFFFu));
-    return act8_round(f, act8_scale(e), e);
+template <class E> __device__ __forceinline__ void act8_write(const Act8Piece<E>& p, E* v, int left) {
+    if (left >= 8) {
+        __builtin_memcpy(v, p.raw, sizeof(p.raw));
+    } else {
+#pragma unroll
+        for (int k = 0; k < 7; ++k)
+            if (k < left) Elem<E>::store(v + k, p.value(k));
+    }
+}
+// Rounding: held to +-127 (which rounds to itself, so that it may come first), 1.5 2^23 added: the sum's last byte is the nearest whole number, halves to even,
+// in two's complement, and its one rounding is that of v 2^(133 - e).  Restoring: a byte plus 128 is converted without a sign
+// (one instruction a byte) and 128 taken off again (before the product: 128 steps may be past the largest number).
+template <class E> __device__ __forceinline__ u32x2_t act8_pack(const Act8Piece<E>& p, uint32_t& e) {
+    e = act8_exponent(quad_max_u32(p.top()));
+    const float scale = act8_scale(e);
+    uint32_t b[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) b[k] = __float_as_uint(__builtin_amdgcn_fmed3f(p.value(k) * scale, -127.0f, 127.0f) + 12582912.0f);
+    const uint32_t keep = e == 255 ? 0u : 0xFFFFFFFFu;
+    u32x2_t w;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t lo = __builtin_amdgcn_perm(b[4 * h + 1], b[4 * h], 0x0C0C0400u), hi = __builtin_amdgcn_perm(b[4 * h + 3], b[4 * h + 2], 0x0C0C0400u);
+        w[h] = __builtin_amdgcn_perm(hi, lo, 0x05040100u) & keep;
+    }
+    return w;
+}
+template <class E> __device__ __forceinline__ void act8_unpack(u32x2_t w, uint32_t e, Act8Piece<E>& p) {
+    const float step = act8_step(e);
+    w ^= 0x80808080u;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) p.set(k, ((float)((w[k / 4] >> (k % 4 * 8)) & 0xFFu) - 128.0f) * step);
+}
+__device__ __forceinline__ u32x2_t act8_read_bytes(const int8_t* q, int left) {
+    u32x2_t w{0, 0};
+    if (left >= 8) {
+        __builtin_memcpy(&w, q, 8);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 7; ++k)
+            if (k < left) w[k / 4] |= (uint32_t)(uint8_t)q[k] << (k % 4 * 8);
+    }
+    return w;
+}
+__device__ __forceinline__ void act8_write_bytes(u32x2_t w, int8_t* q, int left) {
+    if (left >= 8) {
+        __builtin_memcpy(q, &w, 8);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 7; ++k)
+            if (k < left) q[k] = (int8_t)(w[k / 4] >> (k % 4 * 8));
+    }
 }
 
-// One workgroup per token.  A step takes 2048 values of x (256, where rows are not whole pieces) and 1024 slots: everything it reads is
-// asked for before anything is worked on, so that a row of the usual sizes costs one trip to memory.  The mask is put together in LDS.
-// Entries of idx outside [0, F) are ignored.
-constexpr int kAct8Slots = 4;      // of a thread in a step
-template <class E, bool VEC>
+// Where piece p of a token's x, gate and up values is: n values, at `v` and `q` from their row's start, their block's byte at `e`.
+template <class V> struct Act8At {
+    V* v;
+    int8_t* q;
+    uint8_t* e;
+    int left;      // values from here to the row's end, negative in lanes that only fill a block
+    __device__ __forceinline__ Act8At(int p, const moc_act8_set& s, int64_t t, int d, int K, V* x, V* g, V* u) {
+        const int db = act8_blocks(d), kb = act8_blocks(K);
+        int n = d, blocks = db;
+        v = x, q = s.xq, e = s.xe;
+        if (p >= 4 * db) {
+            p -= 4 * db;
+            n = K, blocks = kb;
+            v = g, q = s.gq, e = s.ge;
+            if (p >= 4 * kb) p -= 4 * kb, v = u, q = s.uq, e = s.ue;
+        }
+        const int64_t at = t * n + p * 8;
+        v += at, q += at;
+        e += t * blocks + p / 4;
+        left = n - p * 8;
+    }
+};
+
+// One workgroup per token.  The pieces of its x, gate and up values are shared out over the threads, two a thread and step, and asked for together; the mask is put
+// together in LDS.  Entries of idx outside [0, F) are ignored.
+constexpr int kAct8Ahead = 2, kAct8Idx = 4;
+template <class E>
 __global__ __launch_bounds__(256) void act8_save_kernel(const E* __restrict__ x, const int32_t* __restrict__ idx, const E* __restrict__ g, const E* __restrict__ u, int d, int F,
                                                         int K, moc_act8_set set) {
     extern __shared__ uint32_t act8_words[];
     const int64_t t = blockIdx.x;
-    const int tid = threadIdx.x, words = act8_blocks(F), db = act8_blocks(d), kb = act8_blocks(K);
-    constexpr int XSTEP = VEC ? 2048 : 256, KSTEP = 256 * kAct8Slots;
-    const int xend = db * kAct8Block, kend = kb * kAct8Block;      // whole blocks: their lanes stay together
+    const int tid = threadIdx.x, words = act8_blocks(F), pieces = 4 * (act8_blocks(d) + 2 * act8_blocks(K));
     for (int i = tid; i < words; i += 256) act8_words[i] = 0;
-    for (int x0 = 0, k0 = 0; x0 < d || k0 < K; x0 += XSTEP, k0 += KSTEP) {
-        const int xi = x0 + tid * (VEC ? 8 : 1);
-        Act8Piece<E> piece;
-        float one = 0.0f, gv[kAct8Slots], uv[kAct8Slots];
-        int ch[kAct8Slots];
-        if (VEC) piece.load(x + t * d + xi, xi < d);
-        else if (xi < d) one = Elem<E>::load(x + t * d + xi);
+    int ch[kAct8Idx];
 #pragma unroll
-        for (int q = 0; q < kAct8Slots; ++q) {
-            const int s = k0 + q * 256 + tid;
-            ch[q] = s < K ? idx[t * K + s] : -1;
-            gv[q] = s < K ? Elem<E>::load(g + t * K + s) : 0.0f;
-            uv[q] = s < K ? Elem<E>::load(u + t * K + s) : 0.0f;
+    for (int i = 0; i < kAct8Idx; ++i) ch[i] = tid + 256 * i < K ? idx[t * K + tid + 256 * i] : -1;
+    const auto mark = [&](int j) {
+        if (j >= 0 && j < F) atomicOr(&act8_words[j >> 5], 1u << (j & 31));
+    };
+    for (int p0 = 0; p0 < pieces; p0 += 256 * kAct8Ahead) {
+        Act8Piece<E> piece[kAct8Ahead];
+#pragma unroll
+        for (int i = 0; i < kAct8Ahead; ++i) {
+            const int p = p0 + i * 256 + tid;
+            if (p >= pieces) continue;
+            const Act8At<const E> at(p, set, t, d, K, x, g, u);
+            act8_read<E>(piece[i], at.v, at.left);
         }
-        if (x0 == 0) __syncthreads();      // (the words are zero)
-        if (xi < xend) {
+        if (p0 == 0) {
+            __syncthreads();      // (the words are zero)
+#pragma unroll
+            for (int i = 0; i < kAct8Idx; ++i) mark(ch[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < kAct8Ahead; ++i) {
+            const int p = p0 + i * 256 + tid;
+            if (p >= pieces) continue;      // (blocks of 4 lanes stay together)
+            const Act8At<const E> at(p, set, t, d, K, x, g, u);
             uint32_t e;
-            if (VEC) {
-                const u32x2_t w = piece.pack(e);
-                if (xi < d) *reinterpret_cast<u32x2_t*>(set.xq + t * d + xi) = w;
-            } else {
-                const int w = act8_pack_one(one, e);
-                if (xi < d) set.xq[t * d + xi] = (int8_t)w;
-            }
-            if (xi % kAct8Block == 0) set.xe[t * db + xi / kAct8Block] = (uint8_t)e;
-        }
-#pragma unroll
-        for (int q = 0; q < kAct8Slots; ++q) {
-            const int s = k0 + q * 256 + tid;
-            if (s >= kend) continue;
-            if (ch[q] >= 0 && ch[q] < F) atomicOr(&act8_words[ch[q] >> 5], 1u << (ch[q] & 31));
-            uint32_t eg, eu;
-            const int wg = act8_pack_one(gv[q], eg), wu = act8_pack_one(uv[q], eu);
-            if (s < K) {
-                set.gq[t * K + s] = (int8_t)wg;
-                set.uq[t * K + s] = (int8_t)wu;
-            }
-            if (s % kAct8Block == 0) {
-                set.ge[t * kb + s / kAct8Block] = (uint8_t)eg;
-                set.ue[t * kb + s / kAct8Block] = (uint8_t)eu;
-            }
+            const u32x2_t w = act8_pack<E>(piece[i], e);
+            act8_write_bytes(w, at.q, at.left);
+            if ((p & 3) == 0) *at.e = (uint8_t)e;
         }
     }
+    for (int s = tid + 256 * kAct8Idx; s < K; s += 256) mark(idx[t * K + s]);
     __syncthreads();
     for (int i = tid; i < words; i += 256) set.sel[t * words + i] = act8_words[i];
 }
 
-// x of a row from its 8 bits
-template <class E, bool VEC> __device__ __forceinline__ void act8_unpack_row(const int8_t* __restrict__ q, const uint8_t* __restrict__ e, int n, E* __restrict__ v) {
-    if (VEC) {
-        for (int i = threadIdx.x * 8; i < n; i += 256 * 8) act8_unpack_piece<E>(*reinterpret_cast<const u32x2_t*>(q + i), e[i / kAct8Block], v + i);
-    } else {
-        for (int i = threadIdx.x; i < n; i += 256) Elem<E>::store(v + i, (float)q[i] * act8_step(e[i / kAct8Block]));
-    }
-}
-
-// The inverse, with the same steps.  Channels are written in the order of the set bits; a row with fewer than K bits (not one that was saved) leaves the
-// rest of its indices at -1, bits past the K-th are dropped.
-template <class E, bool VEC>
+// The inverse, shared out in the same way.  Channels go to LDS in the order of the set bits, 8192 channels at a time, and from there to memory; a row with fewer
+// than K bits (not one that was saved) leaves the rest of its indices at -1, bits past the K-th are dropped.
+template <class E>
 __global__ __launch_bounds__(256) void act8_load_kernel(moc_act8_set set, int d, int F, int K, E* __restrict__ x, int32_t* __restrict__ idx, E* __restrict__ g, E* __restrict__ u) {
-    __shared__ int sums[2][4];
+    __shared__ int sums[4];
+    __shared__ uint16_t place[256 * 32];
     const int64_t t = blockIdx.x;
-    const int tid = threadIdx.x, words = act8_blocks(F), db = act8_blocks(d), kb = act8_blocks(K), wave = tid >> 6;
-    constexpr int XSTEP = VEC ? 2048 : 256, KSTEP = 256 * kAct8Slots;
-    int base = 0, turn = 0;
-    for (int x0 = 0, k0 = 0, w0 = 0; x0 < d || k0 < K || w0 < words; x0 += XSTEP, k0 += KSTEP, w0 += 256, turn ^= 1) {
-        const int xi = x0 + tid * (VEC ? 8 : 1), w = w0 + tid;
+    const int tid = threadIdx.x, words = act8_blocks(F), pieces = 4 * (act8_blocks(d) + 2 * act8_blocks(K)), wave = tid >> 6;
+    const auto word = [&](int w) {
         uint32_t bits = w < words ? set.sel[t * words + w] : 0;
-        u32x2_t xw{0, 0};
-        uint32_t xe = 0;
-        float one = 0.0f, gv[kAct8Slots], uv[kAct8Slots];
-        uint32_t ge[kAct8Slots], ue[kAct8Slots];
-        if (xi < d) {
-            if (VEC) xw = *reinterpret_cast<const u32x2_t*>(set.xq + t * d + xi);
-            else one = (float)set.xq[t * d + xi];
-            xe = set.xe[t * db + xi / kAct8Block];
+        if (w == words - 1 && (F & 31)) bits &= (1u << (F & 31)) - 1;
+        return bits;
+    };
+    uint32_t bits = word(tid);
+    for (int p0 = 0; p0 < pieces; p0 += 256 * kAct8Ahead) {
+        u32x2_t w[kAct8Ahead];
+        uint32_t e[kAct8Ahead];
+#pragma unroll
+        for (int i = 0; i < kAct8Ahead; ++i) {
+            const int p = p0 + i * 256 + tid;
+            if (p >= pieces) continue;
+            const Act8At<E> at(p, set, t, d, K, x, g, u);
+            w[i] = act8_read_bytes(at.q, at.left);
+            e[i] = *at.e;
         }
 #pragma unroll
-        for (int q = 0; q < kAct8Slots; ++q) {
-            const int s = k0 + q * 256 + tid;
-            gv[q] = s < K ? (float)set.gq[t * K + s] : 0.0f;
-            uv[q] = s < K ? (float)set.uq[t * K + s] : 0.0f;
-            ge[q] = s < K ? set.ge[t * kb + s / kAct8Block] : 0u;
-            ue[q] = s < K ? set.ue[t * kb + s / kAct8Block] : 0u;
+        for (int i = 0; i < kAct8Ahead; ++i) {
+            const int p = p0 + i * 256 + tid;
+            if (p >= pieces) continue;
+            const Act8At<E> at(p, set, t, d, K, x, g, u);
+            Act8Piece<E> piece;
+            act8_unpack<E>(w[i], e[i], piece);
+            act8_write<E>(piece, at.v, at.left);
         }
-        if (w0 < words) {
-            if (w == words - 1 && (F & 31)) bits &= (1u << (F & 31)) - 1;
-            const int mine = __popc(bits), upto = wave_inclusive_sum(mine);
-            if ((tid & 63) == 63) sums[turn][wave] = upto;
-            __syncthreads();
-            int at = base + upto - mine;
-            for (int i = 0; i < wave; ++i) at += sums[turn][i];
-            base += sums[turn][0] + sums[turn][1] + sums[turn][2] + sums[turn][3];
-            for (; bits != 0 && at < K; bits &= bits - 1) idx[t * K + at++] = w * 32 + __ffs(bits) - 1;
-        }
-        if (xi < d) {
-            if (VEC) act8_unpack_piece<E>(xw, xe, x + t * d + xi);
-            else Elem<E>::store(x + t * d + xi, one * act8_step(xe));
-        }
-#pragma unroll
-        for (int q = 0; q < kAct8Slots; ++q) {
-            const int s = k0 + q * 256 + tid;
-            if (s >= K) continue;
-            Elem<E>::store(g + t * K + s, gv[q] * act8_step(ge[q]));
-            Elem<E>::store(u + t * K + s, uv[q] * act8_step(ue[q]));
-        }
+    }
+    int base = 0;
+    for (int w0 = 0; w0 < words; w0 += 256) {
+        if (w0 > 0) bits = word(w0 + tid);
+        const int mine = __popc(bits), upto = wave_inclusive_sum(mine);
+        if ((tid & 63) == 63) sums[wave] = upto;
+        __syncthreads();
+        int at = upto - mine;
+        for (int i = 0; i < wave; ++i) at += sums[i];
+        const int n = sums[0] + sums[1] + sums[2] + sums[3];
+        for (; bits != 0; bits &= bits - 1) place[at++] = (uint16_t)(tid * 32 + __ffs(bits) - 1);
+        __syncthreads();
+        for (int s = tid; s < min(n, K - base); s += 256) idx[t * K + base + s] = w0 * 32 + place[s];
+        base += n;
     }
     for (int s = base + tid; s < K; s += 256) idx[t * K + s] = -1;
 }
@@ -214,10 +261,12 @@ __global__ __launch_bounds__(256) void bwd_expand_act8_kernel(moc_act8_set set, 
     constexpr int PER16 = 16 / sizeof(E), SLOTS = kAct8Span / 64, BATCH = 4;
     __shared__ __align__(16) E span[4][3][kAct8Span];
     if ((int)blockIdx.x < unpack_groups) {
-        for (int64_t t = blockIdx.x; t < T; t += unpack_groups) {
-            if (d % 8 == 0) act8_unpack_row<E, true>(set.xq + t * d, set.xe + t * act8_blocks(d), d, x + t * d);
-            else act8_unpack_row<E, false>(set.xq + t * d, set.xe + t * act8_blocks(d), d, x + t * d);
-        }
+        for (int64_t t = blockIdx.x; t < T; t += unpack_groups)
+            for (int i = threadIdx.x * 8; i < d; i += 256 * 8) {
+                Act8Piece<E> piece;
+                act8_unpack<E>(act8_read_bytes(set.xq + t * d + i, d - i), set.xe[t * act8_blocks(d) + i / kAct8Block], piece);
+                act8_write<E>(piece, x + t * d + i, d - i);
+            }
         return;
     }
     // (the wavefront's number is the same in all its lanes: what follows from it stays out of the vector registers)

@@ -17,14 +17,12 @@ moc_status check_width(const moc_shape* shape) {
 template <class E> void save(const Dims& D, const E* x, const int32_t* idx, const E* g, const E* u, const moc_act8_set& set, hipStream_t st) {
     Span span("act8_save", st);
     const size_t lds = (size_t)act8_blocks(D.F) * 4;
-    auto kern = D.d % 8 == 0 ? act8_save_kernel<E, true> : act8_save_kernel<E, false>;
-    hipLaunchKernelGGL(kern, dim3(D.T), dim3(256), lds, st, x, idx, g, u, D.d, D.F, D.K, set);
+    hipLaunchKernelGGL((act8_save_kernel<E>), dim3(D.T), dim3(256), lds, st, x, idx, g, u, D.d, D.F, D.K, set);
 }
 
 template <class E> void load(const Dims& D, const moc_act8_set& set, E* x, int32_t* idx, E* g, E* u, hipStream_t st) {
     Span span("act8_load", st);
-    auto kern = D.d % 8 == 0 ? act8_load_kernel<E, true> : act8_load_kernel<E, false>;
-    hipLaunchKernelGGL(kern, dim3(D.T), dim3(256), 0, st, set, D.d, D.F, D.K, x, idx, g, u);
+    hipLaunchKernelGGL((act8_load_kernel<E>), dim3(D.T), dim3(256), 0, st, set, D.d, D.F, D.K, x, idx, g, u);
 }
 
 }  // namespace
