@@ -8,7 +8,6 @@ using namespace mocapi;
 namespace {
 
 constexpr int kMaxNormDim = 16384;      // 64 elements in each of 256 lanes, 32 in each of 512
-constexpr int kNormGroups = 256;        // most workgroups of a backward launch, one a compute unit: rows of `part`
 
 moc_status check_norm(int32_t T, int32_t d, int32_t dtype) {
     if (T < 1 || d < 1) return fail(MOC_ERR_BAD_ARG, "T and d must be >= 1 (got %d, %d)", T, d);
@@ -17,31 +16,41 @@ moc_status check_norm(int32_t T, int32_t d, int32_t dtype) {
     return MOC_OK;
 }
 
-// Whether rows of d elements all start on 16 bytes.
-template <class E> bool rows_aligned(int d) { return d % Vec16<E>::N == 0; }
+template <RowForm F> struct Form { static constexpr RowForm value = F; };
 
-// f(pieces of W elements, their number NV, lanes of a row): the fewest lanes that hold d elements with at most EL, or twice as many
-// in rows past that, in each.
-template <class E, int EL, int MIN, int MAX, class F> void for_row(int d, int least, const F& f) {
-    constexpr int V = Vec16<E>::N;
-    if constexpr (MIN < MAX) {
-        if (MIN < least || d > MIN * EL) return for_row<E, EL, 2 * MIN, MAX>(d, least, f);
+// f(form of the rows, pieces of a lane, lanes of a row) for the fewest lanes, MIN .. MAX and at least `least`, that hold d
+// elements in NV pieces each; a wavefront's rows that fill a half or a quarter of that take NV / 2 or NV / 4, rows past MAX lanes 2 or 4 times as many.
+template <class E, int NV, int MIN, int MAX, class F> void for_row(int d, int least, const F& f) {
+    constexpr int W = Vec16<E>::N, EL = NV * W;
+    const auto with = [&](auto nv) {
+        const std::integral_constant<int, MIN> lanes{};
+        if (d % W == 0) f(Form<RowForm::Whole>{}, nv, lanes);
+        else f(Form<RowForm::Odd>{}, nv, lanes);
+    };
+    if constexpr (MIN == 64) {
+        if (d < W) return f(Form<RowForm::Narrow>{}, std::integral_constant<int, 1>{}, std::integral_constant<int, 64>{});
     }
-    typedef std::integral_constant<int, MIN> Lanes;
-    const bool aligned = rows_aligned<E>(d), once = d <= MIN * EL;
-    if (aligned && once) f(std::integral_constant<int, V>{}, std::integral_constant<int, EL / V>{}, Lanes{});
-    else if (once) f(std::integral_constant<int, 1>{}, std::integral_constant<int, EL>{}, Lanes{});
-    if constexpr (MIN == MAX) {
-        if (aligned && !once) f(std::integral_constant<int, V>{}, std::integral_constant<int, 2 * EL / V>{}, Lanes{});
-        else if (!once) f(std::integral_constant<int, 1>{}, std::integral_constant<int, 2 * EL>{}, Lanes{});
+    if constexpr (MIN < MAX) {
+        if (MIN < least || d > MIN * EL) return for_row<E, NV, 2 * MIN, MAX>(d, least, f);
+        if constexpr (MIN == 64 && NV >= 4) {
+            if (d <= MIN * EL / 4) return with(std::integral_constant<int, NV / 4>{});
+            if (d <= MIN * EL / 2) return with(std::integral_constant<int, NV / 2>{});
+        }
+        with(std::integral_constant<int, NV>{});
+    } else {
+        if (d <= MIN * EL) return with(std::integral_constant<int, NV>{});
+        if constexpr (MIN * EL < kMaxNormDim) {
+            if (d <= 2 * MIN * EL) return with(std::integral_constant<int, 2 * NV>{});
+        }
+        if constexpr (2 * MIN * EL < kMaxNormDim) with(std::integral_constant<int, 4 * NV>{});
     }
 }
 
 template <class E> moc_status layernorm(int T, int d, const E* h, const E* gain, const E* bias, float eps, E* out, hipStream_t st) {
     Span span("layernorm", st);
-    for_row<E, 32, 64, 256>(d, T < 1024 ? 256 : 64, [&](auto W, auto NV, auto TPR) {
+    for_row<E, 16 / Vec16<E>::N, 64, 256>(d, T < 1024 ? 256 : 64, [&](auto form, auto NV, auto TPR) {
         constexpr int rows = 256 / TPR;
-        hipLaunchKernelGGL((layernorm_kernel<E, W, NV, TPR>), dim3((T + rows - 1) / rows), dim3(256), 0, st, h, gain, bias, eps, T, d, out);
+        hipLaunchKernelGGL((layernorm_kernel<E, decltype(form)::value, NV, TPR>), dim3((unsigned)(((int64_t)T + rows - 1) / rows)), dim3(256), 0, st, h, gain, bias, eps, T, d, out);
     });
     HIP_TRY(hipGetLastError());
     return MOC_OK;
@@ -52,11 +61,10 @@ moc_status norm_bwd(int T, int d, const E* h, const E* gain, float eps, const E*
     int groups = 0;
     {
         Span span(RMS ? "rmsnorm_bwd" : "layernorm_bwd", st);
-        for_row<E, 16, 64, 512>(d, 64, [&](auto W, auto NV, auto TPR) {
-            constexpr int threads = 512, rows = threads / TPR;
-            groups = std::min(kNormGroups, (T + rows - 1) / rows);
-            hipLaunchKernelGGL((norm_bwd_kernel<E, W, NV, TPR, threads, RMS, BIAS>), dim3(groups), dim3(threads), 0, st, h, gain, eps, dy, dres, T, d, dh, part, dgain,
-                               dbias);
+        for_row<E, 4, 64, 512>(d, 64, [&](auto form, auto NV, auto TPR) {
+            constexpr int rows = kNormThreads / TPR;
+            groups = (int)std::min<int64_t>(kNormGroups, ((int64_t)T + rows - 1) / rows);
+            hipLaunchKernelGGL((norm_bwd_kernel<E, decltype(form)::value, NV, TPR, RMS, BIAS>), dim3(groups), dim3(kNormThreads), 0, st, h, gain, eps, dy, dres, T, d, dh, part, dgain, dbias);
         });
     }
     HIP_TRY(hipGetLastError());

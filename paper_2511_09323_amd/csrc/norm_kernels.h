@@ -5,29 +5,72 @@
 // RMSNorm's dh lacks mean(p).  Everything is fp32; the variance is the mean of squared differences from the mean (a sum of squares
 // would lose a mean that is large against the spread); dh, out, dgain and dbias are rounded once.
 //
-// All of it is bound by memory, so every row is read once: TPR lanes hold it in registers, as NV pieces of W elements each (W = 16
-// bytes' worth where rows are 16-byte aligned, else 1), and the statistics are computed again in the backward pass instead of being
-// stored.  TPR = 64 needs no barrier; more lanes are for long rows, and for few of them.
+// All of it is bound by memory, so every row is read once: TPR lanes hold it in registers, as NV pieces of 16 bytes each, and the
+// statistics are computed again in the backward pass instead of being stored.
 #pragma once
 #include "common.h"
 #include "misc_kernels.h"
 
 namespace moc {
 
-template <class E, int W> struct Piece {
-    static_assert(W == Vec16<E>::N, "16 bytes, or one element (below)");
-    typedef u32x4_t Raw;
-    static __device__ __forceinline__ Raw zero() { return u32x4_t{0, 0, 0, 0}; }
-    static __device__ __forceinline__ Raw load(const E* p) { return *reinterpret_cast<const u32x4_t*>(p); }
-    static __device__ __forceinline__ void unpack(Raw r, float* v) { Vec16<E>::unpack(r, v); }
-    static __device__ __forceinline__ void store(E* p, const float* v) { *reinterpret_cast<u32x4_t*>(p) = Vec16<E>::pack(v); }
-};
-template <class E> struct Piece<E, 1> {
-    typedef E Raw;
-    static __device__ __forceinline__ Raw zero() { return E(0); }
-    static __device__ __forceinline__ Raw load(const E* p) { return *p; }
-    static __device__ __forceinline__ void unpack(Raw r, float* v) { v[0] = Elem<E>::load(&r); }
-    static __device__ __forceinline__ void store(E* p, const float* v) { Elem<E>::store(p, v[0]); }
+// How the pieces of a row lie.  A load stands in no branch: behind one, the compiler cannot count what is still on its way and waits for everything.
+//   Whole    rows are whole pieces; pieces past a row's end read as zero (buffer loads check the bound);
+//   Odd      any d from a piece's width W on: the last piece is the row's last W elements, and those of them that the piece before it has are
+//            zeroed; pieces past the end read that, too, and are zeroed;
+//   Narrow   d < W: element by element.
+enum class RowForm { Whole, Odd, Narrow };
+
+template <class E, RowForm FORM, int NV, int TPR> struct Row {
+    static constexpr int W = Vec16<E>::N;
+    int d, lane;
+    __device__ __forceinline__ int at(int u) const { return (u * TPR + lane) * W; }                             // the piece's first column
+    __device__ __forceinline__ int first(int u) const { return FORM == RowForm::Odd ? min(at(u), d - W) : at(u); }      // the column of its element 0
+    // whether some lane's piece u is not W elements of its own (uniform)
+    __device__ __forceinline__ bool ragged(int u) const { return FORM != RowForm::Whole && (u + 1) * TPR * W > d; }
+    __device__ __forceinline__ bool has(int u, int e) const { return first(u) + e >= at(u) && first(u) + e < d; }
+    // Row t of p (t the same in a wavefront), or zeros where `in` is false; p has T rows.
+    __device__ __forceinline__ void load(const E* p, int64_t t, int T, bool in, u32x4_t* raw) const {
+        if (FORM == RowForm::Whole) {
+            const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<E*>(p + (in ? t * d : 0)), 0, in ? (uint32_t)d * sizeof(E) : 0u, 0x00020000);
+#pragma unroll
+            for (int u = 0; u < NV; ++u) raw[u] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rsrc, (u * TPR + lane) * 16, 0, 0));
+        } else if (FORM == RowForm::Odd) {
+            const E* row = p + (in ? t : (int64_t)T - 1) * d;
+#pragma unroll
+            for (int u = 0; u < NV; ++u) __builtin_memcpy(&raw[u], row + first(u), 16);
+        } else {
+            float v[W];
+#pragma unroll
+            for (int e = 0; e < W; ++e) v[e] = in && has(0, e) ? Elem<E>::load(p + t * d + e) : 0.0f;
+            raw[0] = Vec16<E>::pack(v);      // (exact: these are E's values)
+        }
+    }
+    // What the loads of an Odd row brought that is not the lane's own becomes zero.  (Apart from the load, which would be waited for.)
+    __device__ __forceinline__ void clean(bool in, u32x4_t* raw) const {
+        if (FORM != RowForm::Odd) return;
+#pragma unroll
+        for (int u = 0; u < NV; ++u) {
+            if (in && !ragged(u)) continue;
+            float v[W];
+            Vec16<E>::unpack(raw[u], v);
+#pragma unroll
+            for (int e = 0; e < W; ++e) v[e] = in && has(u, e) ? v[e] : 0.0f;
+            raw[u] = Vec16<E>::pack(v);
+        }
+    }
+    __device__ __forceinline__ void store(E* row, int u, const float* v) const {
+        if (FORM == RowForm::Whole) {
+            const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(row, 0, (uint32_t)d * sizeof(E), 0x00020000);
+            __builtin_amdgcn_raw_buffer_store_b128(Vec16<E>::pack(v), rsrc, (u * TPR + lane) * 16, 0, 0);
+        } else if (!ragged(u)) {
+            const u32x4_t r = Vec16<E>::pack(v);
+            __builtin_memcpy(row + at(u), &r, 16);
+        } else {
+#pragma unroll
+            for (int e = 0; e < W; ++e)
+                if (has(u, e)) Elem<E>::store(row + first(u) + e, v[e]);
+        }
+    }
 };
 
 // Sum over the TPR lanes of a row, for all of them.  `red` holds the wavefronts' sums; consecutive calls alternate between its two
@@ -50,17 +93,18 @@ struct RowSums {
     }
 };
 
-// mean and 1 / sqrt(variance + eps) of the row whose pieces are in raw (pieces past the row's end are zero).
-template <class E, int W, int NV, int TPR, bool RMS>
-__device__ __forceinline__ void row_stats(const typename Piece<E, W>::Raw* raw, int lane, int d, float eps, RowSums& sums, float& mean, float& r) {
+// mean and 1 / sqrt(variance + eps) of the row whose pieces are in raw.
+template <class E, RowForm FORM, int NV, int TPR, bool RMS>
+__device__ __forceinline__ void row_stats(const Row<E, FORM, NV, TPR>& row, const u32x4_t* raw, float eps, RowSums& sums, float& mean, float& r) {
+    constexpr int W = Vec16<E>::N;
     mean = 0.0f;
-    const float scale = 1.0f / (float)d;
+    const float scale = 1.0f / (float)row.d;
     if (!RMS) {
         float s = 0.0f;
 #pragma unroll
         for (int u = 0; u < NV; ++u) {
             float v[W];
-            Piece<E, W>::unpack(raw[u], v);
+            Vec16<E>::unpack(raw[u], v);
 #pragma unroll
             for (int e = 0; e < W; ++e) s += v[e];
         }
@@ -70,58 +114,63 @@ __device__ __forceinline__ void row_stats(const typename Piece<E, W>::Raw* raw, 
 #pragma unroll
     for (int u = 0; u < NV; ++u) {
         float v[W];
-        Piece<E, W>::unpack(raw[u], v);
-        if (RMS || (u * TPR + lane) * W < d) {
+        Vec16<E>::unpack(raw[u], v);
+        if (RMS || (FORM == RowForm::Whole ? row.at(u) < row.d : !row.ragged(u))) {
 #pragma unroll
             for (int e = 0; e < W; ++e) ss = fmaf(v[e] - mean, v[e] - mean, ss);
+        } else if (FORM != RowForm::Whole) {
+#pragma unroll
+            for (int e = 0; e < W; ++e) ss = row.has(u, e) ? fmaf(v[e] - mean, v[e] - mean, ss) : ss;
         }
     }
     r = 1.0f / sqrtf(sums.sum<TPR>(ss) * scale + eps);
 }
 
 // One row per TPR lanes.  out may be h.
-template <class E, int W, int NV, int TPR>
-__global__ __launch_bounds__(256) void layernorm_kernel(const E* h, const E* __restrict__ gain, const E* __restrict__ bias, float eps, int T, int d,
-                                                        E* out) {
+template <class E, RowForm FORM, int NV, int TPR>
+__global__ __launch_bounds__(256) void layernorm_kernel(const E* h, const E* __restrict__ gain, const E* __restrict__ bias, float eps, int T, int d, E* out) {
+    constexpr int W = Vec16<E>::N;
     __shared__ float red[2][kMaxRowWaves];
     RowSums sums{red};
-    const int lane = threadIdx.x % TPR;
+    const Row<E, FORM, NV, TPR> row{d, (int)threadIdx.x % TPR};
     const int64_t t = (int64_t)blockIdx.x * (256 / TPR) + __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);      // (the same in a whole wavefront)
-    const int width = t < T ? d : 0;      // (rows past the last wait with the others)
-    const E* x = h + t * d;
-    typename Piece<E, W>::Raw raw[NV];
-#pragma unroll
-    for (int u = 0; u < NV; ++u) {
-        const int i = (u * TPR + lane) * W;
-        raw[u] = i < width ? Piece<E, W>::load(x + i) : Piece<E, W>::zero();
-    }
+    const bool in = t < T;      // (rows past the last wait with the others)
+    u32x4_t raw[NV], rg[NV], rb[NV];
+    row.load(h, t, T, in, raw);
+    row.load(gain, 0, 1, true, rg);
+    row.load(bias ? bias : gain, 0, 1, true, rb);
+    row.clean(in, raw);
     float mean, r;
-    row_stats<E, W, NV, TPR, false>(raw, lane, d, eps, sums, mean, r);
+    row_stats<E, FORM, NV, TPR, false>(row, raw, eps, sums, mean, r);
+    if (!in) return;
 #pragma unroll
     for (int u = 0; u < NV; ++u) {
-        const int i = (u * TPR + lane) * W;
-        if (i >= width) continue;
         float v[W], g[W], b[W];
-        Piece<E, W>::unpack(raw[u], v);
-        Piece<E, W>::unpack(Piece<E, W>::load(gain + i), g);
-        Piece<E, W>::unpack(bias ? Piece<E, W>::load(bias + i) : Piece<E, W>::zero(), b);
+        Vec16<E>::unpack(raw[u], v);
+        Vec16<E>::unpack(rg[u], g);
+        Vec16<E>::unpack(bias ? rb[u] : u32x4_t{0, 0, 0, 0}, b);
 #pragma unroll
         for (int e = 0; e < W; ++e) v[e] = fmaf((v[e] - mean) * r, g[e], b[e]);
-        Piece<E, W>::store(out + t * d + i, v);
+        row.store(out + t * d, u, v);
     }
 }
 
-// Backward: every TPR lanes walk over rows and add dy n and dy up in registers; a workgroup's sums are joined in LDS and written as
-// one row of `part` ([workgroup][dgain, dbias][d]), or, where there is a single workgroup, to dgain and dbias themselves.  dh may
-// be dy or dres: an element is read by the lane that writes it.
-template <class E, int W, int NV, int TPR, int THREADS, bool RMS, bool BIAS>
-__global__ __launch_bounds__(THREADS) void norm_bwd_kernel(const E* __restrict__ h, const E* __restrict__ gain, float eps, const E* dy, const E* dres, int T, int d, E* dh,
-                                                           float* __restrict__ part, E* __restrict__ dgain, E* __restrict__ dbias) {
-    constexpr int ROWS = THREADS / TPR;
+// Backward: one workgroup a compute unit; every TPR lanes walk over rows, with the next row on its way while one is worked on, and add dy n and
+// dy up in registers.  (Loads come back in order, so nothing that is needed sooner is asked for after the next row: the gain is in LDS.)
+// A workgroup's sums are joined in LDS and written as one row of `part` ([workgroup][dgain, dbias][d]), or, where there is a single
+// workgroup, to dgain and dbias themselves.  dh may be dy or dres: an element is read by the lane that writes it, or before, by the lane beside it.
+constexpr int kNormThreads = 512;
+template <class E, RowForm FORM, int NV, int TPR, bool RMS, bool BIAS>
+__global__ __launch_bounds__(kNormThreads) void norm_bwd_kernel(const E* __restrict__ h, const E* __restrict__ gain, float eps, const E* dy, const E* dres, int T, int d, E* dh,
+                                                                float* __restrict__ part, E* __restrict__ dgain, E* __restrict__ dbias) {
+    constexpr int W = Vec16<E>::N, ROWS = kNormThreads / TPR;
+    constexpr bool AHEAD = NV <= 4;      // (more pieces leave no registers for a second row)
     __shared__ float red[2][kMaxRowWaves];
     __shared__ float join[ROWS == 1 ? 1 : ROWS][ROWS == 1 ? 1 : TPR * W];
+    __shared__ u32x4_t gains[AHEAD ? NV * TPR : 1];
     RowSums sums{red};
-    const int lane = threadIdx.x % TPR, slot = __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);      // (the same in a whole wavefront)
+    const Row<E, FORM, NV, TPR> row{d, (int)threadIdx.x % TPR};
+    const int lane = row.lane, slot = __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);      // (the same in a whole wavefront)
     const float scale = 1.0f / (float)d;
     float ag[NV * W], ab[BIAS ? NV * W : 1];
 #pragma unroll
@@ -130,27 +179,47 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(const E* __restrict__
 #pragma unroll
         for (int i = 0; i < NV * W; ++i) ab[i] = 0.0f;
     }
+    u32x4_t rh[NV], ry[NV], nh[NV], ny[NV];
+    const int64_t step = (int64_t)gridDim.x * ROWS;
     // (every lane goes through the same number of rows: sums over more than a wavefront synchronise the workgroup)
-    for (int64_t t0 = (int64_t)blockIdx.x * ROWS; t0 < T; t0 += (int64_t)gridDim.x * ROWS) {
-        const int64_t t = t0 + slot;
-        const int width = t < T ? d : 0;
-        typename Piece<E, W>::Raw rh[NV], ry[NV];
+    int64_t t0 = (int64_t)blockIdx.x * ROWS;
+    if (AHEAD) {
+        u32x4_t g[NV];
+        row.load(gain, 0, 1, true, g);
+        row.load(h, t0 + slot, T, t0 + slot < T, nh);
+        row.load(dy, t0 + slot, T, t0 + slot < T, ny);
+        if (slot == 0) {
 #pragma unroll
-        for (int u = 0; u < NV; ++u) {
-            const int i = (u * TPR + lane) * W;
-            rh[u] = i < width ? Piece<E, W>::load(h + t * d + i) : Piece<E, W>::zero();
-            ry[u] = i < width ? Piece<E, W>::load(dy + t * d + i) : Piece<E, W>::zero();
+            for (int u = 0; u < NV; ++u) gains[u * TPR + lane] = g[u];
         }
+        __syncthreads();
+    }
+    for (; t0 < T; t0 += step) {
+        const int64_t t = t0 + slot, next = t + step;
+        const bool in = t < T;
+        u32x4_t rr[NV], rg[NV];
+        if (dres) row.load(dres, t, T, in, rr);
+        if (AHEAD) {
+#pragma unroll
+            for (int u = 0; u < NV; ++u) rh[u] = nh[u], ry[u] = ny[u];
+            row.load(h, next, T, next < T, nh);
+            row.load(dy, next, T, next < T, ny);
+        } else {
+            row.load(h, t, T, in, rh);
+            row.load(dy, t, T, in, ry);
+            row.load(gain, 0, 1, true, rg);
+        }
+        row.clean(in, rh);
+        row.clean(in, ry);
         float mean, r;
-        row_stats<E, W, NV, TPR, RMS>(rh, lane, d, eps, sums, mean, r);
+        row_stats<E, FORM, NV, TPR, RMS>(row, rh, eps, sums, mean, r);
         float sp = 0.0f, spn = 0.0f;
 #pragma unroll
         for (int u = 0; u < NV; ++u) {
-            const int i = (u * TPR + lane) * W;
             float x[W], y[W], g[W];
-            Piece<E, W>::unpack(rh[u], x);
-            Piece<E, W>::unpack(ry[u], y);
-            Piece<E, W>::unpack(i < d ? Piece<E, W>::load(gain + i) : Piece<E, W>::zero(), g);
+            Vec16<E>::unpack(rh[u], x);
+            Vec16<E>::unpack(ry[u], y);
+            Vec16<E>::unpack(AHEAD ? gains[u * TPR + lane] : rg[u], g);
 #pragma unroll
             for (int e = 0; e < W; ++e) {
                 const float n = (x[e] - mean) * r, p = y[e] * g[e];      // (past the row's end y and p are zero)
@@ -161,21 +230,20 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(const E* __restrict__
             }
         }
         const float m1 = RMS ? 0.0f : sums.sum<TPR>(sp) * scale, m2 = sums.sum<TPR>(spn) * scale;
+        if (!in) continue;
 #pragma unroll
         for (int u = 0; u < NV; ++u) {
-            const int i = (u * TPR + lane) * W;
-            if (i >= width) continue;
             float x[W], y[W], g[W], o[W];
-            Piece<E, W>::unpack(rh[u], x);
-            Piece<E, W>::unpack(ry[u], y);
-            Piece<E, W>::unpack(Piece<E, W>::load(gain + i), g);
-            Piece<E, W>::unpack(dres ? Piece<E, W>::load(dres + t * d + i) : Piece<E, W>::zero(), o);
+            Vec16<E>::unpack(rh[u], x);
+            Vec16<E>::unpack(ry[u], y);
+            Vec16<E>::unpack(AHEAD ? gains[u * TPR + lane] : rg[u], g);
+            Vec16<E>::unpack(dres ? rr[u] : u32x4_t{0, 0, 0, 0}, o);
 #pragma unroll
             for (int e = 0; e < W; ++e) {
                 const float n = (x[e] - mean) * r;
                 o[e] = fmaf(r, fmaf(-n, m2, fmaf(y[e], g[e], -m1)), o[e]);
             }
-            Piece<E, W>::store(dh + t * d + i, o);
+            row.store(dh + t * d, u, o);
         }
     }
     // the workgroup's sums, columns of one piece at a time
@@ -189,19 +257,21 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(const E* __restrict__
 #pragma unroll
         for (int u = 0; u < NV; ++u) {
             if (ROWS == 1) {
-                const int i = (u * TPR + lane) * W;
-                if (i >= d) continue;
 #pragma unroll
                 for (int e = 0; e < W; ++e) {
-                    if (last) Elem<E>::store(out + i + e, a[u * W + e]);
-                    else mine[q * d + i + e] = a[u * W + e];
+                    if (!row.has(u, e)) continue;
+                    const int i = row.first(u) + e;
+                    if (last) Elem<E>::store(out + i, a[u * W + e]);
+                    else mine[q * d + i] = a[u * W + e];
                 }
             } else {
+                if (u * TPR * W >= d) break;      // (uniform)
                 __syncthreads();
 #pragma unroll
-                for (int e = 0; e < W; ++e) join[slot][lane * W + e] = a[u * W + e];
+                for (int e = 0; e < W; ++e)
+                    if (row.has(u, e)) join[slot][row.first(u) + e - u * TPR * W] = a[u * W + e];
                 __syncthreads();
-                for (int c = threadIdx.x; c < TPR * W; c += THREADS) {
+                for (int c = threadIdx.x; c < TPR * W; c += kNormThreads) {
                     const int i = u * TPR * W + c;
                     if (i >= d) continue;
                     float s = 0.0f;
@@ -215,17 +285,22 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(const E* __restrict__
     }
 }
 
-// Sums over the workgroups' rows of `part`, in their order: 64 columns and 16 shares of the rows a workgroup.
+// Sums over the workgroups' rows of `part`, in their order: 64 columns and 16 shares of the rows a workgroup; a share's rows are asked for together.
+constexpr int kNormGroups = 256;        // most workgroups of a backward launch, one a compute unit: rows of `part`
 template <class E>
 __global__ __launch_bounds__(1024) void norm_bwd_join_kernel(const float* __restrict__ part, int rows, int64_t cols, int d, E* __restrict__ dgain, E* __restrict__ dbias) {
     __shared__ float sums[16][64];
-    const int lane = threadIdx.x & 63, share = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, share = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t c = (int64_t)blockIdx.x * 64 + lane;
-    float s = 0.0f;
-    if (c < cols) {
-#pragma unroll 4
-        for (int p = share; p < rows; p += 16) s += part[p * cols + c];
+    float v[kNormGroups / 16];
+#pragma unroll
+    for (int i = 0; i < kNormGroups / 16; ++i) {
+        const int p = share + 16 * i;
+        v[i] = p < rows && c < cols ? part[p * cols + c] : 0.0f;
     }
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kNormGroups / 16; ++i) s += v[i];
     sums[share][lane] = s;
     __syncthreads();
     if (share != 0 || c >= cols) return;
