@@ -261,8 +261,10 @@ __global__ __launch_bounds__(256) void bwd_expand_act8_kernel(moc_act8_set set, 
     constexpr int PER16 = 16 / sizeof(E), SLOTS = kAct8Span / 64, BATCH = 4;
     __shared__ __align__(16) E span[4][3][kAct8Span];
     if ((int)blockIdx.x < unpack_groups) {
-        for (int64_t t = blockIdx.x; t < T; t += unpack_groups)
-            for (int i = threadIdx.x * 8; i < d; i += 256 * 8) {
+        // (a row a wavefront)
+        for (int64_t t = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); t < T; t += unpack_groups * 4)
+#pragma unroll 4
+            for (int i = (threadIdx.x & 63) * 8; i < d; i += 64 * 8) {
                 Act8Piece<E> piece;
                 act8_unpack<E>(act8_read_bytes(set.xq + t * d + i, d - i), set.xe[t * act8_blocks(d) + i / kAct8Block], piece);
                 act8_write<E>(piece, x + t * d + i, d - i);

@@ -152,7 +152,11 @@ struct Args {
         ok = ok && t->dim() == 2 && t->size(1) <= INT32_MAX;
         return ok ? (int32_t)t->size(1) : 0;
     }
-    static int device() { return c10::hip::getCurrentHIPStream().device_index(); }
+    int dev = -1;
+    int device() {
+        if (dev < 0) dev = c10::hip::getCurrentHIPStream().device_index();
+        return dev;
+    }
     // experts + 1 row offsets from a list or tuple of integers
     int32_t* offsets(int i, int32_t* buf, int cap) {
         if (!ok || !(PyList_CheckExact(v[i]) || PyTuple_CheckExact(v[i])) || experts + 1 > cap || PySequence_Fast_GET_SIZE(v[i]) != experts + 1) {
@@ -406,7 +410,7 @@ struct Act8Bwd {
         wg = a.weight(w), wu = a.weight(w + 1), wd = a.weight(w + 2);
         dx = a.act(w + 4), dwg = a.weight(w + 5), dwu = a.weight(w + 6), dwd = a.weight(w + 7);
         ws = a.scratch(w + 8, &n);
-        for (int k = w; k < w + 8; ++k) a.ok = a.ok && THPVariable_Unpack(a.v[k]).device().index() == Args::device();
+        for (int k = w; k < w + 8; ++k) a.ok = a.ok && THPVariable_Unpack(a.v[k]).device().index() == a.device();
     }
 };
 

@@ -29,8 +29,8 @@ struct RouteWs {
         chunk = std::max(route_threads(lanes) / lanes, (T + kRouteGroups - 1) / kRouteGroups);
         groups = (T + chunk - 1) / chunk;
         Carver c(ws);
-        hist = c.take<int32_t>((size_t)groups * (E + 1));
-        psum = c.take<float>((size_t)groups * E);
+        hist = c.take<int32_t>((size_t)route_pad(groups) * (E + 1));
+        psum = c.take<float>((size_t)route_pad(groups) * E);
         bytes = c.off;
     }
 };
@@ -49,7 +49,10 @@ template <class E> moc_status route(const E* logits, const RouteArgs& a, hipStre
         Span span("route_rows", st);
         for_token<E>(a.E, [&](auto L, auto vec) {
             constexpr int threads = route_threads(L);
-            hipLaunchKernelGGL((route_rows_kernel<E, L, vec>), dim3(a.groups), dim3(threads), route_rows_words(a.E, threads, a.groups == 1) * 4, st, logits, a);
+            if (a.groups == 1)
+                hipLaunchKernelGGL((route_rows_kernel<E, L, vec, true>), dim3(1), dim3(threads), route_rows_words(a.E, threads, true) * 4, st, logits, a);
+            else
+                hipLaunchKernelGGL((route_rows_kernel<E, L, vec, false>), dim3(a.groups), dim3(threads), route_rows_words(a.E, threads, false) * 4, st, logits, a);
         });
     }
     HIP_TRY(hipGetLastError());

@@ -166,7 +166,8 @@ __global__ __launch_bounds__(kNormThreads) void norm_bwd_kernel(const E* __restr
     constexpr int W = Vec16<E>::N, ROWS = kNormThreads / TPR;
     constexpr bool AHEAD = NV <= 4;      // (more pieces leave no registers for a second row)
     __shared__ float red[2][kMaxRowWaves];
-    __shared__ float join[ROWS == 1 ? 1 : ROWS][ROWS == 1 ? 1 : TPR * W];
+    constexpr int PASS = NV < 16 / W ? NV : 16 / W;      // 32 KB of LDS
+    __shared__ float join[ROWS == 1 ? 1 : ROWS][ROWS == 1 ? 1 : PASS * TPR * W];
     __shared__ u32x4_t gains[AHEAD ? NV * TPR : 1];
     RowSums sums{red};
     const Row<E, FORM, NV, TPR> row{d, (int)threadIdx.x % TPR};
@@ -246,7 +247,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_bwd_kernel(const E* __restr
             row.store(dh + t * d, u, o);
         }
     }
-    // the workgroup's sums, columns of one piece at a time
+    // the workgroup's sums, PASS pieces of a lane at a time
     const bool last = gridDim.x == 1;
     constexpr int SUMS = BIAS ? 2 : 1;
     float* mine = part + (int64_t)blockIdx.x * SUMS * d;
@@ -254,32 +255,34 @@ __global__ __launch_bounds__(kNormThreads) void norm_bwd_kernel(const E* __restr
     for (int q = 0; q < SUMS; ++q) {
         const float* a = q ? ab : ag;
         E* const out = q ? dbias : dgain;
+        const auto result = [&](int i, float s) {
+            if (last) Elem<E>::store(out + i, s);
+            else mine[q * d + i] = s;
+        };
+        if (ROWS == 1) {
 #pragma unroll
-        for (int u = 0; u < NV; ++u) {
-            if (ROWS == 1) {
-#pragma unroll
-                for (int e = 0; e < W; ++e) {
-                    if (!row.has(u, e)) continue;
-                    const int i = row.first(u) + e;
-                    if (last) Elem<E>::store(out + i, a[u * W + e]);
-                    else mine[q * d + i] = a[u * W + e];
-                }
-            } else {
-                if (u * TPR * W >= d) break;      // (uniform)
-                __syncthreads();
+            for (int u = 0; u < NV; ++u)
 #pragma unroll
                 for (int e = 0; e < W; ++e)
-                    if (row.has(u, e)) join[slot][row.first(u) + e - u * TPR * W] = a[u * W + e];
-                __syncthreads();
-                for (int c = threadIdx.x; c < TPR * W; c += kNormThreads) {
-                    const int i = u * TPR * W + c;
-                    if (i >= d) continue;
-                    float s = 0.0f;
+                    if (row.has(u, e)) result(row.first(u) + e, a[u * W + e]);
+            continue;
+        }
 #pragma unroll
-                    for (int w = 0; w < ROWS; ++w) s += join[w][c];
-                    if (last) Elem<E>::store(out + i, s);
-                    else mine[q * d + i] = s;
-                }
+        for (int u0 = 0; u0 < NV; u0 += PASS) {
+            const int c0 = u0 * TPR * W;
+            if (c0 >= d) break;      // (uniform)
+            __syncthreads();
+#pragma unroll
+            for (int u = u0; u < u0 + PASS; ++u)
+#pragma unroll
+                for (int e = 0; e < W; ++e)
+                    if (row.has(u, e)) join[slot][row.first(u) + e - c0] = a[u * W + e];
+            __syncthreads();
+            for (int c = threadIdx.x; c < min(PASS * TPR * W, d - c0); c += kNormThreads) {
+                float s = 0.0f;
+#pragma unroll
+                for (int w = 0; w < ROWS; ++w) s += join[w][c];
+                result(c0 + c, s);
             }
         }
     }

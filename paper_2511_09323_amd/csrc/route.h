@@ -40,6 +40,23 @@ template <int L, class T, class Op> __device__ __forceinline__ T token_reduce(T 
     }
     return v;
 }
+// Sum over a wavefront's tokens, lane by lane of a token: every lane gets that of the lanes congruent to it modulo L.  (Register moves as in wave_reduce, stopped
+// at L.)
+template <int L> __device__ __forceinline__ float column_sum(float v) {
+    {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    if (L <= 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    if (L <= 8) v += dpp_move<0x128>(v);      // row_ror 8, 4, 2, 1
+    if (L <= 4) v += dpp_move<0x124>(v);
+    if (L <= 2) v += dpp_move<0x122>(v);
+    if (L <= 1) v += dpp_move<0x121>(v);
+    return v;
+}
 struct OpSum { template <class T> __device__ __forceinline__ T operator()(T a, T b) const { return a + b; } };
 struct OpMax { template <class T> __device__ __forceinline__ T operator()(T a, T b) const { return a > b ? a : b; } };
 struct OpMin { template <class T> __device__ __forceinline__ T operator()(T a, T b) const { return a < b ? a : b; } };
@@ -71,6 +88,45 @@ template <int L, class F> __device__ __forceinline__ void route_slots(int k, con
     }
 }
 
+// Choosing one expert after the other.  fp32: the largest key (common.h), then the lowest expert that has it.  bf16 leaves half of a key's bits free for the
+// expert's number, inverted, so that one reduction finds both (about 25 instructions a slot instead of 60).  A NaN is below everything, an expert that
+// was chosen, too.
+template <class E> struct RouteKeys;
+template <> struct RouteKeys<float> {
+    uint32_t key[kRoutePer];
+    __device__ __forceinline__ void set(int i, int, float l) { key[i] = l == l ? float_key(l) : 0u; }
+    template <int L> __device__ __forceinline__ int take(int e0, float& value, bool& above) {      // the expert, its logit, whether that is above -inf
+        uint32_t best = 0;
+        int at = 0;
+#pragma unroll
+        for (int i = 0; i < kRoutePer; ++i)
+            if (key[i] > best) best = key[i], at = i;
+        const uint32_t top = token_reduce<L>(best, OpMax());
+        const int e = token_reduce<L>(best == top ? e0 + at : INT32_MAX, OpMin());
+#pragma unroll
+        for (int i = 0; i < kRoutePer; ++i) key[i] = e0 + i == e ? 0u : key[i];
+        value = key_float(top);
+        above = top > float_key(-INFINITY);
+        return e;
+    }
+};
+template <> struct RouteKeys<bf16_t> {
+    uint32_t key[kRoutePer];
+    __device__ __forceinline__ void set(int i, int e, float l) { key[i] = l == l ? (float_key(l) & 0xFFFF0000u) | (0xFFFFu - e) : 0u; }
+    template <int L> __device__ __forceinline__ int take(int, float& value, bool& above) {
+        uint32_t best = 0;
+#pragma unroll
+        for (int i = 0; i < kRoutePer; ++i) best = max(best, key[i]);
+        const uint32_t top = token_reduce<L>(best, OpMax());
+#pragma unroll
+        for (int i = 0; i < kRoutePer; ++i) key[i] = key[i] == top ? 0u : key[i];
+        const uint32_t h = top >> 16;
+        value = __uint_as_float(h & 0x8000u ? (h & 0x7FFFu) << 16 : ~top & 0xFFFF0000u);
+        above = h > (float_key(-INFINITY) >> 16);
+        return (int)(0xFFFFu - (top & 0xFFFFu));
+    }
+};
+
 struct RouteArgs {
     int T, E, k, chunk, groups;      // tokens of a workgroup, workgroups
     bool renorm;
@@ -79,37 +135,65 @@ struct RouteArgs {
     float* weights;
     int32_t *counts, *order;
     float *loss, *coef;
-    // by workgroup: copies of every expert, then tokens with a slot; and the sum of p over the tokens
-    int32_t* hist;                   // [groups, E + 1]
-    float* psum;                     // [groups, E]
+    // by workgroup (rows of route_pad(groups)): copies of every expert, then tokens with a slot; and the sum of p over the tokens
+    int32_t* hist;                   // [E + 1][groups]
+    float* psum;                     // [E][groups]
 };
 
-// Threads share out `groups` rows of values for E experts: thread tid takes expert tid % width of the rows part, part + parts, ...
+__device__ __forceinline__ int round_up_64(int n) { return (n + 63) & ~63; }
+
+// Sums over the workgroups: an expert's numbers lie side by side ([expert][workgroup]), `lanes` neighbouring threads (4 .. 64) share them out in fours.
+constexpr int kRouteOrderThreads = 1024;
 struct RouteShare {
-    int e, part, parts, width;
+    int lanes, e, at;
     __device__ __forceinline__ RouteShare(int E) {
-        const int bits = 32 - __clz((E - 1) | 1);           // 2^bits >= E
-        width = 1 << bits;
-        e = threadIdx.x & (width - 1);
-        part = threadIdx.x >> bits;
-        parts = blockDim.x >> bits;
+        const int bits = 32 - __clz((E - 1) | 1), log = min(6, 10 - bits);      // 2^bits >= E, 2^10 threads
+        lanes = 1 << log;
+        e = threadIdx.x >> log;
+        at = (threadIdx.x & (lanes - 1)) * 4;
+    }
+    template <class T> __device__ __forceinline__ T sum(T v) const {
+        for (int o = 1; o < lanes; o <<= 1) v += __shfl_xor(v, o, 64);
+        return v;
+    }
+};
+inline __host__ __device__ int route_pad(int groups) { return (groups + 3) & ~3; }
+
+// Running sums of up to 256 experts' copies (LDS), by every wavefront for itself: no barrier.
+struct RouteScan {
+    static constexpr int N = kMaxRouteExperts / 64;
+    int before[N], total = 0;      // lane l: the copies of the experts before 64 c + l
+    __device__ __forceinline__ RouteScan(const int* count, int experts) {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int c = 0; c < N; ++c) {
+            before[c] = 0;
+            if (c * 64 >= experts) continue;
+            const int n = c * 64 + lane < experts ? count[c * 64 + lane] : 0, upto = wave_inclusive_sum(n);
+            before[c] = total + upto - n;
+            total += __builtin_amdgcn_readlane(upto, 63);
+        }
+    }
+    // Of expert e, all of a wavefront's in the same 64.
+    __device__ __forceinline__ int operator()(int e) const {
+        int v = 0;
+#pragma unroll
+        for (int c = 0; c < N; ++c)
+            if (__builtin_amdgcn_readfirstlane(e >> 6) == c) v = __shfl(before[c], e & 63, 64);
+        return v;
     }
 };
 
-// The loss, its derivative and the counts, by the first wavefront, from every expert's copies, the tokens with a slot (count[E]) and the
-// sums of p: `parts` rows of `width` sums.
-template <class F> __device__ __forceinline__ void route_loss(const RouteArgs& a, const int* count, const F* psum, int parts, int width) {
-    const int tid = threadIdx.x;
-    if (tid >= 64) return;
-    int A = 0;
-    for (int e = tid; e < a.E; e += 64) A += count[e];
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) A += __shfl_xor(A, o, 64);
+// The loss, its derivative and the counts, by one wavefront, from every expert's copies, the tokens with a slot (count[E]) and the
+// sums of p: `rows` rows of E.
+template <class F> __device__ __forceinline__ void route_loss(const RouteArgs& a, const int* count, const F* psum, int rows) {
+    const int tid = threadIdx.x & 63;
+    const int A = RouteScan(count, a.E).total;
     const double scale = A > 0 ? (double)a.E / ((double)A * (double)count[a.E]) : 0.0;
     double loss = 0.0;
     for (int e = tid; e < a.E; e += 64) {
         double p = 0.0;
-        for (int q = 0; q < parts; ++q) p += (double)psum[q * width + e];
+        for (int q = 0; q < rows; ++q) p += (double)psum[q * a.E + e];
         if (A > 0) loss += scale * count[e] * p;
         a.counts[e] = count[e];
         a.coef[e] = (float)(scale * count[e]);
@@ -119,36 +203,8 @@ template <class F> __device__ __forceinline__ void route_loss(const RouteArgs& a
     if (tid == 0) a.loss[0] = (float)loss;
 }
 
-// The places of the copies of tokens t0 .. t0 + n - 1 (n <= 256), whose experts are in `ids` (of copy tid + THREADS * i): a bit per token and expert gives
-// every copy the number of those before it.  base[e] (LDS): the place of expert e's first one, moved on behind its last.  `mask`, `place`: LDS, 8 E words each;
-// mask is zero, and again after the call.
+// Places of copies: a bit per token (of 256) and expert gives every copy the number of those before it.  A thread holds the experts of copies tid + THREADS * i.
 constexpr int route_copies(int threads) { return 256 * kMaxRouteSlots / threads; }
-template <int THREADS> __device__ __forceinline__ void route_places(const RouteArgs& a, int t0, int n, const int* ids, int* base, uint32_t* mask, int* place) {
-    const int tid = threadIdx.x;
-#pragma unroll
-    for (int i = 0; i < route_copies(THREADS); ++i) {
-        const int c = tid + THREADS * i, t = c / a.k;
-        if (c < n * a.k && ids[i] >= 0) atomicOr(&mask[ids[i] * 8 + (t >> 5)], 1u << (t & 31));
-    }
-    __syncthreads();
-    for (int i = tid; i < 8 * a.E; i += THREADS) {
-        int at = base[i >> 3];
-        for (int w = i & ~7; w < i; ++w) at += __popc(mask[w]);
-        place[i] = at;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < route_copies(THREADS); ++i) {
-        const int c = tid + THREADS * i, t = c / a.k;
-        if (c >= n * a.k || ids[i] < 0) continue;
-        const int at = ids[i] * 8 + (t >> 5);
-        a.order[place[at] + __popc(mask[at] & ((1u << (t & 31)) - 1))] = t0 * a.k + c;
-    }
-    for (int e = tid; e < a.E; e += THREADS) base[e] = place[e * 8 + 7] + __popc(mask[e * 8 + 7]);
-    __syncthreads();
-    for (int i = tid; i < 8 * a.E; i += THREADS) mask[i] = 0;
-    __syncthreads();
-}
 template <int THREADS> __device__ __forceinline__ void route_ids(const RouteArgs& a, int t0, int n, int* ids) {
 #pragma unroll
     for (int i = 0; i < route_copies(THREADS); ++i) {
@@ -156,93 +212,123 @@ template <int THREADS> __device__ __forceinline__ void route_ids(const RouteArgs
         ids[i] = c < n * a.k ? a.ids[(int64_t)t0 * a.k + c] : -1;
     }
 }
-// base[e] += the copies of the experts before e, for up to 256 experts whose copies are in all[]; the result is their sum over all experts.  `waves`: LDS, 4 words.
-__device__ __forceinline__ int route_bases(int experts, const int* all, int* base, int* waves) {
-    const int tid = threadIdx.x;
-    int upto = 0, n = 0;
-    if (tid < 256) {
-        n = tid < experts ? all[tid] : 0;
-        upto = wave_inclusive_sum(n);
-        if ((tid & 63) == 63) waves[tid >> 6] = upto;
+template <int THREADS> __device__ __forceinline__ void route_mark(const RouteArgs& a, const int* ids, uint32_t* mask) {
+#pragma unroll
+    for (int i = 0; i < route_copies(THREADS); ++i) {
+        const int t = (threadIdx.x + THREADS * i) / a.k;
+        if (ids[i] >= 0) atomicOr(&mask[ids[i] * 8 + (t >> 5)], 1u << (t & 31));
     }
-    __syncthreads();
-    if (tid < experts) {
-        for (int w = 0; w < (tid >> 6); ++w) upto += waves[w];
-        base[tid] += upto - n;
-    }
-    __syncthreads();
-    return waves[0] + waves[1] + waves[2] + waves[3];
+}
+// the copies of mask word i's expert in the words before it
+__device__ __forceinline__ int route_before(const uint32_t* mask, int i) {
+    int n = 0;
+    for (int w = i & ~7; w < i; ++w) n += __popc(mask[w]);
+    return n;
 }
 
-// Second launch.  A workgroup places its own copies; the last workgroup does the loss.
-constexpr int kRouteOrderThreads = 1024;
+// Second launch.  A workgroup places its own copies, behind those of the workgroups before it; the last workgroup does the loss.
 static __global__ __launch_bounds__(kRouteOrderThreads) void route_order_kernel(RouteArgs a) {
     constexpr int THREADS = kRouteOrderThreads;
-    __shared__ int all[kMaxRouteExperts + 1], base[kMaxRouteExperts], waves[4];
-    __shared__ __align__(16) uint32_t mem[2 * THREADS > 16 * kMaxRouteExperts ? 2 * THREADS : 16 * kMaxRouteExperts];
-    const int tid = threadIdx.x, group = blockIdx.x;
+    __shared__ int all[kMaxRouteExperts + 1], base[kMaxRouteExperts];
+    __shared__ __align__(16) uint32_t mem[16 * kMaxRouteExperts];
+    const int tid = threadIdx.x, group = blockIdx.x, ld = route_pad(a.groups);
     const RouteShare sh(a.E);
+    typedef int32_t Four __attribute__((ext_vector_type(4)));
     if (group == a.groups) {
         double* psum = reinterpret_cast<double*>(mem);
-        for (int i = tid; i <= a.E; i += THREADS) all[i] = 0;
-        __syncthreads();
+        int n = 0, tokens = 0;
         double p = 0.0;
         if (sh.e < a.E) {
-            int n = 0;
 #pragma unroll 4
-            for (int g = sh.part; g < a.groups; g += sh.parts) {
-                n += a.hist[g * (a.E + 1) + sh.e];
-                p += (double)a.psum[g * a.E + sh.e];
+            for (int g = sh.at; g < a.groups; g += 4 * sh.lanes) {
+                const Four h = *reinterpret_cast<const Four*>(a.hist + sh.e * ld + g);
+                const f32x4_t q = *reinterpret_cast<const f32x4_t*>(a.psum + sh.e * ld + g);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    n += g + i < a.groups ? h[i] : 0;
+                    p += g + i < a.groups ? (double)q[i] : 0.0;
+                }
             }
-            atomicAdd(&all[sh.e], n);
         }
-        psum[tid] = p;
-        for (int g = tid; g < a.groups; g += THREADS) atomicAdd(&all[a.E], a.hist[g * (a.E + 1) + a.E]);
+        if (tid < a.groups) tokens = a.hist[a.E * ld + tid];      // (kRouteGroups <= THREADS)
+        if (tid == 0) all[a.E] = 0;
+        n = sh.sum(n);
+        p = sh.sum(p);
+        if (sh.e < a.E && sh.at == 0) all[sh.e] = n, psum[sh.e] = p;
         __syncthreads();
-        route_loss(a, all, psum, sh.parts, sh.width);
+        if (tid < a.groups) atomicAdd(&all[a.E], tokens);
+        __syncthreads();
+        if (tid < 64) route_loss(a, all, psum, 1);
         return;
     }
+    uint32_t* mask = mem;
+    int* place = reinterpret_cast<int*>(mem) + 8 * a.E;
     const int t0 = group * a.chunk, t1 = (int)min((int64_t)a.T, (int64_t)t0 + a.chunk);
     int ids[route_copies(THREADS)];
     route_ids<THREADS>(a, t0, min(256, t1 - t0), ids);
     // copies of every expert in all workgroups, and in those before this one
     int n = 0, before = 0;
     if (sh.e < a.E) {
-#pragma unroll 8
-        for (int g = sh.part; g < a.groups; g += sh.parts) {
-            const int h = a.hist[g * (a.E + 1) + sh.e];
-            n += h;
-            before += g < group ? h : 0;
+#pragma unroll 4
+        for (int g = sh.at; g < a.groups; g += 4 * sh.lanes) {
+            const Four h = *reinterpret_cast<const Four*>(a.hist + sh.e * ld + g);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                n += g + i < a.groups ? h[i] : 0;
+                before += g + i < group ? h[i] : 0;
+            }
         }
     }
-    for (int i = tid; i < a.E; i += THREADS) base[i] = all[i] = 0;
-    for (int i = tid; i < 8 * a.E; i += THREADS) mem[i] = 0;
+    for (int i = tid; i < 8 * a.E; i += THREADS) mask[i] = 0;
+    n = sh.sum(n);
+    before = sh.sum(before);
+    if (sh.e < a.E && sh.at == 0) all[sh.e] = n, base[sh.e] = before;
     __syncthreads();
-    if (sh.e < a.E) {
-        atomicAdd(&all[sh.e], n);
-        atomicAdd(&base[sh.e], before);
-    }
+    route_mark<THREADS>(a, ids, mask);
     __syncthreads();
-    const int A = route_bases(a.E, all, base, waves);
+    const RouteScan scan(all, a.E);
     for (int t = t0; t < t1; t += 256) {
-        if (t > t0) route_ids<THREADS>(a, t, min(256, t1 - t), ids);
-        route_places<THREADS>(a, t, min(256, t1 - t), ids, base, mem, reinterpret_cast<int*>(mem) + 8 * a.E);
+        if (t > t0) {
+            route_ids<THREADS>(a, t, min(256, t1 - t), ids);
+            for (int i = tid; i < 8 * a.E; i += THREADS) mask[i] = 0;
+            __syncthreads();
+            route_mark<THREADS>(a, ids, mask);
+            __syncthreads();
+        }
+        for (int i = tid; i < round_up_64(8 * a.E); i += THREADS) {      // (whole wavefronts)
+            const int first = t == t0 ? scan(i >> 3) : 0;
+            if (i < 8 * a.E) place[i] = base[i >> 3] + first + route_before(mask, i);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < route_copies(THREADS); ++i) {
+            const int c = tid + THREADS * i, u = c / a.k;
+            if (ids[i] < 0) continue;
+            const int at = ids[i] * 8 + (u >> 5);
+            a.order[place[at] + __popc(mask[at] & ((1u << (u & 31)) - 1))] = t * a.k + c;
+        }
+        if (t + 256 >= t1) break;
+        for (int e = tid; e < a.E; e += THREADS) base[e] = place[e * 8 + 7] + __popc(mask[e * 8 + 7]);
+        __syncthreads();
     }
-    for (int64_t i = (int64_t)A + group * THREADS + tid; i < (int64_t)a.T * a.k; i += (int64_t)a.groups * THREADS) a.order[i] = -1;
+    for (int64_t i = (int64_t)scan.total + group * THREADS + tid; i < (int64_t)a.T * a.k; i += (int64_t)a.groups * THREADS) a.order[i] = -1;
 }
 
-// First launch, and the only one where a workgroup holds all tokens (a.groups = 1).  LDS: the wavefronts' sums of p, the histogram (E + 1 words), and for a single
-// workgroup the places.
+// First launch, and (ONE) the only one where one pass of one workgroup does: its copies' places come from the same bits, out of the registers that hold their
+// experts.  LDS: the wavefronts' sums of p, the histogram (E + 1 words), and for a single workgroup the bits and the places.
 constexpr int route_threads(int L) { return L >= 4 ? 1024 : 256 * L; }
-constexpr int route_rows_words(int E, int threads, bool one) { return (threads / 64) * E + E + 1 + (one ? 17 * E + 4 : 0); }
-template <class E, int L, bool VEC> __global__ __launch_bounds__(route_threads(L)) void route_rows_kernel(const E* __restrict__ logits, RouteArgs a) {
+constexpr int route_rows_words(int E, int threads, bool one) { return (threads / 64) * E + E + 1 + (one ? 16 * E : 0); }
+template <class E, int L, bool VEC, bool ONE> __global__ __launch_bounds__(route_threads(L)) void route_rows_kernel(const E* __restrict__ logits, RouteArgs a) {
     extern __shared__ __align__(16) uint32_t route_smem[];
     constexpr int THREADS = route_threads(L), WAVES = THREADS / 64, TOKENS = THREADS / L, REGS = route_regs<L>();
     float* sums = reinterpret_cast<float*>(route_smem);                  // [WAVES, E]
     int* hist = reinterpret_cast<int*>(route_smem) + WAVES * a.E;        // [E + 1]
     const int lane = threadIdx.x % L, slot = threadIdx.x / L, e0 = lane * kRoutePer, wave = threadIdx.x >> 6;
-    for (int i = threadIdx.x; i <= a.E; i += THREADS) hist[i] = 0;
+    uint32_t* mask = route_smem + WAVES * a.E + a.E + 1;                  // [E, 8], ONE
+    int* place = reinterpret_cast<int*>(mask) + 8 * a.E;
+    for (int i = threadIdx.x; i < (ONE ? 9 * a.E + 1 : a.E + 1); i += THREADS) hist[i] = 0;      // (the mask follows)
     __syncthreads();
+    int mine_e[REGS];
     float acc[kRoutePer];
 #pragma unroll
     for (int i = 0; i < kRoutePer; ++i) acc[i] = 0.0f;
@@ -253,36 +339,26 @@ template <class E, int L, bool VEC> __global__ __launch_bounds__(route_threads(L
         float l[kRoutePer], ex[kRoutePer];
         route_logits<E, VEC>(logits + (int64_t)t * a.E, e0, a.E, l);
         bool used = !a.valid || a.valid[t] != 0;
-        // keys: larger logits are larger, a NaN is below everything
-        uint32_t key[kRoutePer];
+        RouteKeys<E> keys;
 #pragma unroll
-        for (int i = 0; i < kRoutePer; ++i) key[i] = l[i] == l[i] ? float_key(l[i]) : 0u;
-        const uint32_t floor_key = float_key(-INFINITY);
+        for (int i = 0; i < kRoutePer; ++i) keys.set(i, e0 + i, l[i]);
         float top = 0.0f, chosen = 0.0f, all = 1.0f, mine_x[REGS];
-        int mine_e[REGS];
         route_slots<L>(a.k, [&](int r, int holder, int j) {
-            uint32_t best = 0;
-            int at = 0;
-#pragma unroll
-            for (int i = 0; i < kRoutePer; ++i)
-                if (key[i] > best) best = key[i], at = i;
-            const uint32_t row = token_reduce<L>(best, OpMax());
-            const int e = token_reduce<L>(best == row ? e0 + at : INT32_MAX, OpMin());
-            const bool live = used && row > floor_key;
+            float logit;
+            bool above;
+            const int e = keys.template take<L>(e0, logit, above);
+            const bool live = used && above;
             if (j == 0) {
                 used = live;
-                top = key_float(row);
+                top = logit;
                 float s = 0.0f;
 #pragma unroll
                 for (int i = 0; i < kRoutePer; ++i) ex[i] = live && e0 + i < a.E ? expf(l[i] - top) : 0.0f, s += ex[i];
                 all = token_reduce<L>(s, OpSum());
             }
-            const float x = live ? expf(key_float(row) - top) : 0.0f;
+            const float x = live ? expf(logit - top) : 0.0f;
             chosen += x;
             if (lane == holder) mine_e[r] = live ? e : -1, mine_x[r] = x;
-#pragma unroll
-            for (int i = 0; i < kRoutePer; ++i)
-                if (e0 + i == e) key[i] = 0;
         });
         const float by = used ? (a.renorm ? chosen : all) : 1.0f, den = used ? 1.0f / all : 0.0f;
 #pragma unroll
@@ -291,7 +367,9 @@ template <class E, int L, bool VEC> __global__ __launch_bounds__(route_threads(L
             if (j >= a.k) continue;
             a.ids[(int64_t)t * a.k + j] = mine_e[r];
             a.weights[(int64_t)t * a.k + j] = mine_x[r] / by;
-            if (mine_e[r] >= 0) atomicAdd(&hist[mine_e[r]], 1);
+            if (mine_e[r] < 0) continue;
+            atomicAdd(&hist[mine_e[r]], 1);
+            if (ONE) atomicOr(&mask[mine_e[r] * 8 + (t >> 5)], 1u << (t & 31));
         }
         if (used && lane == 0) atomicAdd(&hist[a.E], 1);
 #pragma unroll
@@ -300,33 +378,36 @@ template <class E, int L, bool VEC> __global__ __launch_bounds__(route_threads(L
     // the wavefront's tokens, then the wavefronts in LDS
 #pragma unroll
     for (int i = 0; i < kRoutePer; ++i) {
-        float v = acc[i];
-#pragma unroll
-        for (int o = L; o < 64; o <<= 1) v += __shfl_xor(v, o, 64);
+        const float v = column_sum<L>(acc[i]);
         if ((threadIdx.x & 63) < L && e0 + i < a.E) sums[wave * a.E + e0 + i] = v;
     }
-    if (a.groups == 1) {
-        uint32_t* mask = route_smem + WAVES * a.E + a.E + 1;
-        int *place = reinterpret_cast<int*>(mask) + 8 * a.E, *base = place + 8 * a.E, *waves = base + a.E;
-        for (int i = threadIdx.x; i < 8 * a.E; i += THREADS) mask[i] = 0;
-        for (int i = threadIdx.x; i < a.E; i += THREADS) base[i] = 0;
-        __syncthreads();      // (the workgroup's own ids are in memory, too)
-        route_loss(a, hist, sums, WAVES, a.E);
-        int ids[route_copies(THREADS)];
-        route_ids<THREADS>(a, 0, a.T, ids);
-        const int A = route_bases(a.E, hist, base, waves);
-        route_places<THREADS>(a, 0, a.T, ids, base, mask, place);
-        for (int i = A + threadIdx.x; i < a.T * a.k; i += THREADS) a.order[i] = -1;
+    __syncthreads();
+    if (ONE) {
+        const RouteScan scan(hist, a.E);
+        for (int i = threadIdx.x; i < round_up_64(8 * a.E); i += THREADS) {      // (whole wavefronts)
+            const int first = scan(i >> 3);
+            if (i < 8 * a.E) place[i] = first + route_before(mask, i);
+        }
+        __syncthreads();
+        const int t = slot;
+#pragma unroll
+        for (int r = 0; r < REGS; ++r) {
+            const int j = r * L + lane;
+            if (t >= a.T || j >= a.k || mine_e[r] < 0) continue;
+            const int at = mine_e[r] * 8 + (t >> 5);
+            a.order[place[at] + __popc(mask[at] & ((1u << (t & 31)) - 1))] = t * a.k + j;
+        }
+        for (int i = scan.total + threadIdx.x; i < a.T * a.k; i += THREADS) a.order[i] = -1;
+        if (wave == WAVES - 1) route_loss(a, hist, sums, WAVES);
         return;
     }
-    __syncthreads();
     for (int e = threadIdx.x; e < a.E; e += THREADS) {
         float v = 0.0f;
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) v += sums[w * a.E + e];
-        a.psum[group * a.E + e] = v;
+        a.psum[e * route_pad(a.groups) + group] = v;
     }
-    for (int e = threadIdx.x; e <= a.E; e += THREADS) a.hist[group * (a.E + 1) + e] = hist[e];
+    for (int e = threadIdx.x; e <= a.E; e += THREADS) a.hist[e * route_pad(a.groups) + group] = hist[e];
 }
 
 // Gradient of the logits.  A token without a slot gets zeros, whatever its logits are.  dlogits may be logits: a lane writes what it alone read.
