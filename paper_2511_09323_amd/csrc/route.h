@@ -142,12 +142,12 @@ struct RouteArgs {
 
 __device__ __forceinline__ int round_up_64(int n) { return (n + 63) & ~63; }
 
-// Sums over the workgroups: an expert's numbers lie side by side ([expert][workgroup]), `lanes` neighbouring threads (4 .. 64) share them out in fours.
-constexpr int kRouteOrderThreads = 1024;
+// Sums over the workgroups: an expert's numbers lie side by side ([expert][workgroup]), `lanes` neighbouring threads (2 .. 64) share them out in fours.
+constexpr int kRouteOrderLog = 9, kRouteOrderThreads = 1 << kRouteOrderLog;
 struct RouteShare {
     int lanes, e, at;
     __device__ __forceinline__ RouteShare(int E) {
-        const int bits = 32 - __clz((E - 1) | 1), log = min(6, 10 - bits);      // 2^bits >= E, 2^10 threads
+        const int bits = 32 - __clz((E - 1) | 1), log = min(6, kRouteOrderLog - bits);      // 2^bits >= E
         lanes = 1 << log;
         e = threadIdx.x >> log;
         at = (threadIdx.x & (lanes - 1)) * 4;
@@ -226,15 +226,17 @@ __device__ __forceinline__ int route_before(const uint32_t* mask, int i) {
     return n;
 }
 
-// Second launch.  A workgroup places its own copies, behind those of the workgroups before it; the last workgroup does the loss.
+// Second launch.  A workgroup places its own copies, behind those of the workgroups before it.  The loss is the first one's: the last of
+// many starts a few us after it, and the loss takes as long as the places (32768 tokens, 64 experts: 10.3 us with it last, 8.2 with it first; 6.5 with 512 threads a workgroup
+// instead of 1024, of which 256 take longer to start, and 9.5 with 256).
 static __global__ __launch_bounds__(kRouteOrderThreads) void route_order_kernel(RouteArgs a) {
     constexpr int THREADS = kRouteOrderThreads;
     __shared__ int all[kMaxRouteExperts + 1], base[kMaxRouteExperts];
     __shared__ __align__(16) uint32_t mem[16 * kMaxRouteExperts];
-    const int tid = threadIdx.x, group = blockIdx.x, ld = route_pad(a.groups);
+    const int tid = threadIdx.x, group = (int)blockIdx.x - 1, ld = route_pad(a.groups);
     const RouteShare sh(a.E);
     typedef int32_t Four __attribute__((ext_vector_type(4)));
-    if (group == a.groups) {
+    if (group < 0) {
         double* psum = reinterpret_cast<double*>(mem);
         int n = 0, tokens = 0;
         double p = 0.0;
