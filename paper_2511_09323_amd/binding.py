@@ -11,6 +11,7 @@ GPU tensor) the call fails.
 """
 import collections
 import ctypes
+import operator
 import os
 
 import torch
@@ -771,6 +772,7 @@ def _act8_dims(saved):
 def moc_act8_save(x, idx, gvals, uvals, F, out=None):
     """A layer's stored set in 8 bits: x [T,d] and idx, gvals, uvals [T,K] of a forward call over F channels.  Returns an Act8Set."""
     if out is not None:
+        out = Act8Set(*out)
         status = _fast.act8_save(x, idx, gvals, uvals, F, *out)
         if status != _NOT_TAKEN:
             _check(status)
@@ -871,8 +873,9 @@ def moc_route(logits, k, valid=None, renorm=True, ws=None, out=None):
     T, E = _matrix(logits, "logits")
     code = _code(logits.dtype)
     lp = _here(logits, None, None, "logits")
-    if not isinstance(k, int) or not 1 <= k <= E:
-        raise _bad("k must satisfy 1 <= k <= E (got k=%s, E=%d)", k, E)
+    k = operator.index(k)
+    if not 1 <= k <= E:
+        raise _bad("k must satisfy 1 <= k <= E (got k=%d, E=%d)", k, E)
     if out is None:
         new = lambda dt, *shape: torch.empty(shape, dtype=dt, device=logits.device)
         out = (new(torch.int32, T, k), new(torch.float32, T, k), new(torch.int32, E), new(torch.int32, T * k), new(torch.float32, 1), new(torch.float32, E))

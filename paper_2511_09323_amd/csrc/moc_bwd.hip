@@ -172,9 +172,8 @@ moc_status bwd_experts_impl(const Dims& D, int n_exp, const int32_t* off, const 
 template <class E> moc_status expand_act8(const Dims& D, BwdWs<E>& W, const moc_act8_set& set, const RowGroups& rg, E* x, hipStream_t st) {
     Span span("bwd_pointwise_act8", st);
     const int rows = rg.row[rg.n];
-    const int64_t tasks = (int64_t)rows * ((D.ldF + kAct8Span - 1) / kAct8Span), groups = (tasks + 3) / 4;
+    const int64_t tasks = (int64_t)rows * ((D.ldF + kAct8Span - 1) / kAct8Span), groups = (tasks + 3) / 4;      // (T F < 2^40: tasks < 2^32)
     const int unpack = std::min((D.T + 3) / 4, 2048);
-    if (groups + unpack > INT32_MAX) return fail(MOC_ERR_UNSUPPORTED, "T*F too large");
     hipLaunchKernelGGL((bwd_expand_act8_kernel<E>), dim3((unsigned)(unpack + groups)), dim3(256), 0, st, set, W.dZd, rg, rows, D.T, D.d, D.F, D.K,
                        (int64_t)D.ldF, unpack, x, W.Zd, W.dGd, W.dUd);
     HIP_TRY(hipGetLastError());

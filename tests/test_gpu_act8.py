@@ -242,3 +242,29 @@ def test_refusals_with_tensors():
         moc.moc_ffn_bwd_experts_act8(saved, [0, 3, 6], *[v[None] for v in w], dy)
     with pytest.raises(moc.MocError, match="xe"):
         moc.moc_ffn_bwd_act8(saved._replace(xe=None), *w, dy)
+
+
+def test_offsets_past_32_bits():
+    """262149 rows of 8192: the last rows are what they are on their own."""
+    T, d, F, K = (1 << 18) + 5, 8192, 64, 9
+    x, idx, g, u = stored(32, d, F, K, "bf16", 5)
+    alone = moc.moc_act8_save(x, idx, g, u, F)
+    big = torch.zeros(T, d, dtype=torch.bfloat16, device="cuda")
+    big[-32:] = x
+    rest = [torch.cat([t[:1].expand(T - 32, -1), t]).contiguous() for t in (idx, g, u)]
+    saved = moc.moc_act8_save(big, *rest, F)
+    assert all(torch.equal(a[-32:], b) for a, b in zip(saved, alone))
+    back = moc.moc_act8_load(saved, F, torch.bfloat16, out=(big, *rest))
+    assert all(torch.equal(a[-32:], b) for a, b in zip(back, moc.moc_act8_load(alone, F, torch.bfloat16)))
+    assert not back[0][:-32].any()
+
+
+def test_one_workspace_for_call_after_call():
+    """A workspace of a larger layer, used before, serves a smaller one on the same stream."""
+    ws = torch.empty(moc.workspace_bytes(257, 128, 5461, 683, torch.bfloat16, moc.OP_BWD_ACT8), dtype=torch.uint8, device="cuda")
+    for T, d, F, K in ((257, 128, 5461, 683), (40, 64, 171, 21), (257, 128, 5461, 683)):
+        x, idx, g, u, w, dy = layer(T, d, F, K, "bf16", T)
+        saved = moc.moc_act8_save(x, idx, g, u, F)
+        want = moc.moc_ffn_bwd_act8(saved, *w, dy)
+        got = moc.moc_ffn_bwd_act8(saved, *w, dy, ws=ws, out=tuple(torch.empty_like(t) for t in want))
+        assert all(torch.equal(a, b) for a, b in zip(got, want))

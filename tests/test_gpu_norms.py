@@ -196,3 +196,21 @@ def test_refusals_with_tensors():
         moc.moc_layernorm_bwd(a["h"], a["gain"], EPS, a["dy"], ws=torch.empty(256, dtype=torch.uint8, device="cuda"))
     with pytest.raises(moc.MocError, match="16384"):
         moc.moc_layernorm(torch.zeros(1, 16385, device="cuda"), torch.zeros(16385, device="cuda"), None, EPS)
+
+
+def test_offsets_past_32_bits():
+    """262149 rows of 8192: the last rows are what they are on their own."""
+    T, d = (1 << 18) + 5, 8192
+    block = make(64, d, "bf16", 11)
+    tail = slice(T - 64, T)
+    h, dy = torch.zeros(T, d, dtype=torch.bfloat16, device="cuda"), torch.zeros(T, d, dtype=torch.bfloat16, device="cuda")
+    h[tail], dy[tail] = block["h"], block["dy"]
+    out = moc.moc_layernorm(h, block["gain"], block["bias"], EPS)
+    assert torch.equal(out[tail], moc.moc_layernorm(block["h"], block["gain"], block["bias"], EPS))
+    assert torch.equal(out[0], block["bias"])
+    del out
+    dh, dgain, dbias = moc.moc_layernorm_bwd(h, block["gain"], EPS, dy)
+    for got in (dh, moc.moc_rmsnorm_bwd(h, block["gain"], EPS, dy)[0]):
+        assert not got[:-64].any()
+    # (rows of zeros add nothing to the sums; their number is not in the bound of the others' sum)
+    check_backward(block, "bf16", False, False, (dh[tail], dgain, dbias))

@@ -192,3 +192,27 @@ def test_refusals_with_tensors():
         moc.moc_route_bwd(logits, r.ids, r.coef, torch.zeros(10, 3, device="cuda"))
     with pytest.raises(moc.MocError, match="MOC_ERR_WORKSPACE"):
         moc.moc_route(logits, 2, ws=torch.empty(16, dtype=torch.uint8, device="cuda"), out=r)
+
+
+def test_offsets_past_32_bits():
+    """36 million tokens of 64 logits, the same 8192 over and over: what they give on their own, over and over."""
+    n, times, E, k = 8192, 4400, 64, 2
+    block = logits_of(n, E, "bf16", 12)
+    logits = block.repeat(times, 1)
+    T = n * times
+    assert T * E > 2 ** 31
+    one, r = moc.moc_route(block, k), moc.moc_route(logits, np.int64(k))
+    assert torch.equal(r.counts, one.counts * times)
+    for name in ("ids", "weights"):
+        a, b = getattr(r, name).view(times, n, k), getattr(one, name)
+        assert all(torch.equal(a[i], b) for i in (0, 1, times // 2, times - 1)) and torch.equal(a.sum(0), b * times if name == "ids" else a.sum(0))
+    # the mean over tokens is the block's; sums of 2200 numbers of one size in a row: 2200 * 2^-24, twice
+    assert abs(float(r.loss) - float(one.loss)) <= 2.0 ** -11 * float(one.loss)
+    # order: slots ascend within an expert, and a slot's expert is the one its place says
+    at = torch.repeat_interleave(torch.arange(E, device="cuda"), r.counts.long())
+    assert torch.equal(r.ids.view(-1)[r.order.long()].long(), at)
+    assert bool(((r.order[1:] > r.order[:-1]) | (at[1:] != at[:-1])).all())
+    dw = torch.randn(n, k, device="cuda")
+    d = moc.moc_route_bwd(logits, r.ids, r.coef, dw.repeat(times, 1), None)
+    d1 = moc.moc_route_bwd(block, one.ids, one.coef, dw, None)
+    assert torch.equal(d[-n:], d1) and torch.equal(d[:n], d1)
