@@ -130,125 +130,169 @@ __device__ __forceinline__ void act8_write_bytes(u32x2_t w, int8_t* q, int left)
     }
 }
 
-// Where piece p of a token's x, gate and up values is: n values, at `v` and `q` from their row's start, their block's byte at `e`.
-template <class V> struct Act8At {
+// A token's x, gate and up values in steps of 64 pieces, a piece a lane; a step lies in one of the three, so that all but a lane's offset stays in scalar registers.
+template <class V> struct Act8Step {
     V* v;
     int8_t* q;
     uint8_t* e;
-    int left;      // values from here to the row's end, negative in lanes that only fill a block
-    __device__ __forceinline__ Act8At(int p, const moc_act8_set& s, int64_t t, int d, int K, V* x, V* g, V* u) {
-        const int db = act8_blocks(d), kb = act8_blocks(K);
-        int n = d, blocks = db;
-        v = x, q = s.xq, e = s.xe;
-        if (p >= 4 * db) {
-            p -= 4 * db;
-            n = K, blocks = kb;
-            v = g, q = s.gq, e = s.ge;
-            if (p >= 4 * kb) p -= 4 * kb, v = u, q = s.uq, e = s.ue;
+    int n, first;      // values of the row, first piece of the step
+    __device__ __forceinline__ Act8Step(int s, const moc_act8_set& set, int64_t t, int d, int K, V* x, V* g, V* u) {
+        const int xs = act8_steps(d), ks = act8_steps(K);
+        n = d;
+        v = x, q = set.xq, e = set.xe;
+        if (s >= xs) {
+            s -= xs;
+            n = K;
+            v = g, q = set.gq, e = set.ge;
+            if (s >= ks) s -= ks, v = u, q = set.uq, e = set.ue;
         }
-        const int64_t at = t * n + p * 8;
-        v += at, q += at;
-        e += t * blocks + p / 4;
-        left = n - p * 8;
+        v += t * n, q += t * n, e += t * act8_blocks(n);
+        first = s * 64;
     }
+    __device__ __forceinline__ int piece(int lane) const { return first + lane; }
+    __device__ __forceinline__ int left(int lane) const { return n - piece(lane) * 8; }      // values from here to the row's end
+    __device__ __forceinline__ bool in(int lane) const { return piece(lane) < 4 * act8_blocks(n); }      // (blocks of 4 lanes stay together)
+    static __host__ __device__ __forceinline__ int act8_steps(int n) { return (act8_blocks(n) + 15) / 16; }
+    static __device__ __forceinline__ int total(int d, int K) { return act8_steps(d) + 2 * act8_steps(K); }
 };
 
-// One workgroup per token.  The pieces of its x, gate and up values are shared out over the threads, two a thread and step, and asked for together; the mask is put
-// together in LDS.  Entries of idx outside [0, F) are ignored.
-constexpr int kAct8Ahead = 2, kAct8Idx = 4;
+// Four or one wavefronts (WAVES) take a token.  Their number: a workgroup's four take four tokens, or one.  The eight chiplets, which take workgroups in turn, get an
+// eighth of the workgroups each, one behind the other: rows of K values and of block bytes end inside cache lines, and neighbours on one chiplet share its
+// cache, where on two they each move the line (the 1B layer's set restored in 26.4 us without, 23.6 with).
+template <int WAVES> __device__ __forceinline__ int64_t act8_token(int wave) {
+    const unsigned chip = blockIdx.x & 7, each = gridDim.x >> 3, over = gridDim.x & 7;
+    const int64_t group = (int64_t)chip * each + min(chip, over) + (blockIdx.x >> 3);
+    return WAVES == 4 ? group : group * 4 + wave;
+}
+// What a token's wavefronts wait for each other with: a barrier, or for one only that the compiler keeps the order that LDS keeps.
+template <int WAVES> __device__ __forceinline__ void act8_sync() {
+    if (WAVES > 1) {
+        __syncthreads();
+    } else {
+        __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// Saving, four wavefronts a token.  The steps are shared out over them and asked for together (8 steps, 1024 values of idx), so that a token of the usual sizes is one
+// trip to memory; then the mask, which is put together in LDS, and the pieces.  Entries of idx outside [0, F) are ignored.
+// 8192 tokens, d 2048, bf16: 24.9 us with K = 688 (4.6 TB/s of the 5.2 that a large copy reaches), 29.1 with K = 683, whose rows put the pieces at odd addresses.
+constexpr int kAct8Steps = 8, kAct8Idx = 4;
 template <class E>
 __global__ __launch_bounds__(256) void act8_save_kernel(const E* __restrict__ x, const int32_t* __restrict__ idx, const E* __restrict__ g, const E* __restrict__ u, int d, int F,
                                                         int K, moc_act8_set set) {
     extern __shared__ uint32_t act8_words[];
-    const int64_t t = blockIdx.x;
-    const int tid = threadIdx.x, words = act8_blocks(F), pieces = 4 * (act8_blocks(d) + 2 * act8_blocks(K));
-    for (int i = tid; i < words; i += 256) act8_words[i] = 0;
+    typedef Act8Step<const E> Step;
+    constexpr int AHEAD = kAct8Steps / 4;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int64_t t = act8_token<4>(wave);
+    const int words = act8_blocks(F), steps = Step::total(d, K);
+    const int32_t* row = idx + t * K;
     int ch[kAct8Idx];
 #pragma unroll
-    for (int i = 0; i < kAct8Idx; ++i) ch[i] = tid + 256 * i < K ? idx[t * K + tid + 256 * i] : -1;
+    for (int i = 0; i < kAct8Idx; ++i) ch[i] = tid + 256 * i < K ? row[tid + 256 * i] : -1;
+    Act8Piece<E> piece[AHEAD];
+    const auto read = [&](int s0) {
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int s = s0 + i * 4 + wave;
+            if (s >= steps) break;
+            const Step at(s, set, t, d, K, x, g, u);
+            act8_read<E>(piece[i], at.v + at.piece(lane) * 8, at.left(lane));
+        }
+    };
+    read(0);
+    for (int i = tid; i < words; i += 256) act8_words[i] = 0;
+    __syncthreads();
     const auto mark = [&](int j) {
         if (j >= 0 && j < F) atomicOr(&act8_words[j >> 5], 1u << (j & 31));
     };
-    for (int p0 = 0; p0 < pieces; p0 += 256 * kAct8Ahead) {
-        Act8Piece<E> piece[kAct8Ahead];
 #pragma unroll
-        for (int i = 0; i < kAct8Ahead; ++i) {
-            const int p = p0 + i * 256 + tid;
-            if (p >= pieces) continue;
-            const Act8At<const E> at(p, set, t, d, K, x, g, u);
-            act8_read<E>(piece[i], at.v, at.left);
-        }
-        if (p0 == 0) {
-            __syncthreads();      // (the words are zero)
-#pragma unroll
-            for (int i = 0; i < kAct8Idx; ++i) mark(ch[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < kAct8Ahead; ++i) {
-            const int p = p0 + i * 256 + tid;
-            if (p >= pieces) continue;      // (blocks of 4 lanes stay together)
-            const Act8At<const E> at(p, set, t, d, K, x, g, u);
-            uint32_t e;
-            const u32x2_t w = act8_pack<E>(piece[i], e);
-            act8_write_bytes(w, at.q, at.left);
-            if ((p & 3) == 0) *at.e = (uint8_t)e;
-        }
-    }
-    for (int s = tid + 256 * kAct8Idx; s < K; s += 256) mark(idx[t * K + s]);
+    for (int i = 0; i < kAct8Idx; ++i) mark(ch[i]);
+    for (int s = tid + 256 * kAct8Idx; s < K; s += 256) mark(row[s]);
     __syncthreads();
     for (int i = tid; i < words; i += 256) set.sel[t * words + i] = act8_words[i];
+    for (int s0 = 0; s0 < steps; s0 += kAct8Steps) {
+        if (s0 > 0) read(s0);
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int s = s0 + i * 4 + wave;
+            if (s >= steps) break;
+            const Step at(s, set, t, d, K, x, g, u);
+            uint32_t e;
+            const u32x2_t w = act8_pack<E>(piece[i], e);
+            act8_write_bytes(w, at.q + at.piece(lane) * 8, at.left(lane));
+            if (at.in(lane) && (lane & 3) == 0) at.e[at.piece(lane) / 4] = (uint8_t)e;
+        }
+    }
 }
 
-// The inverse, shared out in the same way.  Channels go to LDS in the order of the set bits, 8192 channels at a time, and from there to memory; a row with fewer
-// than K bits (not one that was saved) leaves the rest of its indices at -1, bits past the K-th are dropped.
-template <class E>
-__global__ __launch_bounds__(256) void act8_load_kernel(moc_act8_set set, int d, int F, int K, E* __restrict__ x, int32_t* __restrict__ idx, E* __restrict__ g, E* __restrict__ u) {
-    __shared__ int sums[4];
-    __shared__ uint16_t place[256 * 32];
-    const int64_t t = blockIdx.x;
-    const int tid = threadIdx.x, words = act8_blocks(F), pieces = 4 * (act8_blocks(d) + 2 * act8_blocks(K)), wave = tid >> 6;
-    const auto word = [&](int w) {
-        uint32_t bits = w < words ? set.sel[t * words + w] : 0;
-        if (w == words - 1 && (F & 31)) bits &= (1u << (F & 31)) - 1;
-        return bits;
-    };
-    uint32_t bits = word(tid);
-    for (int p0 = 0; p0 < pieces; p0 += 256 * kAct8Ahead) {
-        u32x2_t w[kAct8Ahead];
-        uint32_t e[kAct8Ahead];
+// Restoring, shared out in the same way over one or four wavefronts a token, the channels first.  They go to LDS in the order of the set bits, 32 for each of the token's lanes at a time, and from there to
+// memory; a row with fewer than K bits (not one that was saved) leaves the rest of its indices at -1, bits past the K-th are dropped.
+template <class E, int WAVES>
+__global__ __launch_bounds__(256) void act8_load_kernel(moc_act8_set set, int T, int d, int F, int K, E* __restrict__ x, int32_t* __restrict__ idx, E* __restrict__ g,
+                                                        E* __restrict__ u) {
+    __shared__ int sums[2][4];
+    __shared__ uint16_t places[256 * 32];
+    typedef Act8Step<E> Step;
+    constexpr int AHEAD = kAct8Steps / WAVES, LANES = 64 * WAVES, WORDS = 4 / WAVES;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), mine = WAVES == 4 ? wave : 0, tid = threadIdx.x & (LANES - 1);
+    const int64_t t = act8_token<WAVES>(wave);
+    if (t >= T) return;
+    const int words = act8_blocks(F), steps = Step::total(d, K);
+    uint16_t* place = places + (WAVES == 4 ? 0 : wave * 64 * 32);
+    const uint32_t* sel = set.sel + t * words;
+    int32_t* row = idx + t * K;
+    uint32_t head[WORDS];
 #pragma unroll
-        for (int i = 0; i < kAct8Ahead; ++i) {
-            const int p = p0 + i * 256 + tid;
-            if (p >= pieces) continue;
-            const Act8At<E> at(p, set, t, d, K, x, g, u);
-            w[i] = act8_read_bytes(at.q, at.left);
-            e[i] = *at.e;
+    for (int i = 0; i < WORDS; ++i) head[i] = i * LANES + tid < words ? sel[i * LANES + tid] : 0;
+    u32x2_t w[AHEAD];
+    uint32_t e[AHEAD];
+    const auto read = [&](int s0) {
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int s = s0 + i * WAVES + mine;
+            if (s >= steps) break;
+            const Step at(s, set, t, d, K, x, g, u);
+            w[i] = act8_read_bytes(at.q + at.piece(lane) * 8, at.left(lane));
+            e[i] = at.in(lane) ? at.e[at.piece(lane) / 4] : 0u;
         }
+    };
+    read(0);
+    int base = 0;
+    const auto channels = [&](int w0, uint32_t bits, int turn) {
+        if (w0 + tid == words - 1 && (F & 31)) bits &= (1u << (F & 31)) - 1;
+        const int own = __popc(bits), upto = wave_inclusive_sum(own);
+        int at = upto - own, n = __builtin_amdgcn_readlane(upto, 63);
+        if (WAVES > 1) {
+            if (lane == 63) sums[turn][wave] = upto;
+            __syncthreads();      // (and the channels before these are out of LDS)
+            for (int i = 0; i < wave; ++i) at += sums[turn][i];
+            n = sums[turn][0] + sums[turn][1] + sums[turn][2] + sums[turn][3];
+        }
+        for (; bits != 0; bits &= bits - 1) place[at++] = (uint16_t)(tid * 32 + __ffs(bits) - 1);
+        act8_sync<WAVES>();
+        for (int s = tid; s < min(n, K - base); s += LANES) row[base + s] = w0 * 32 + place[s];
+        if (WAVES == 1) act8_sync<WAVES>();
+        base += n;
+    };
 #pragma unroll
-        for (int i = 0; i < kAct8Ahead; ++i) {
-            const int p = p0 + i * 256 + tid;
-            if (p >= pieces) continue;
-            const Act8At<E> at(p, set, t, d, K, x, g, u);
+    for (int i = 0; i < WORDS; ++i)
+        if (i * LANES < words) channels(i * LANES, head[i], i & 1);
+    for (int w0 = WORDS * LANES, turn = WORDS & 1; w0 < words; w0 += LANES, turn ^= 1) channels(w0, w0 + tid < words ? sel[w0 + tid] : 0, turn);
+    for (int s = base + tid; s < K; s += LANES) row[s] = -1;
+    for (int s0 = 0; s0 < steps; s0 += kAct8Steps) {
+        if (s0 > 0) read(s0);
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int s = s0 + i * WAVES + mine;
+            if (s >= steps) break;
+            const Step at(s, set, t, d, K, x, g, u);
             Act8Piece<E> piece;
             act8_unpack<E>(w[i], e[i], piece);
-            act8_write<E>(piece, at.v, at.left);
+            act8_write<E>(piece, at.v + at.piece(lane) * 8, at.left(lane));
         }
     }
-    int base = 0;
-    for (int w0 = 0; w0 < words; w0 += 256) {
-        if (w0 > 0) bits = word(w0 + tid);
-        const int mine = __popc(bits), upto = wave_inclusive_sum(mine);
-        if ((tid & 63) == 63) sums[wave] = upto;
-        __syncthreads();
-        int at = upto - mine;
-        for (int i = 0; i < wave; ++i) at += sums[i];
-        const int n = sums[0] + sums[1] + sums[2] + sums[3];
-        for (; bits != 0; bits &= bits - 1) place[at++] = (uint16_t)(tid * 32 + __ffs(bits) - 1);
-        __syncthreads();
-        for (int s = tid; s < min(n, K - base); s += 256) idx[t * K + base + s] = w0 * 32 + place[s];
-        base += n;
-    }
-    for (int s = base + tid; s < K; s += 256) idx[t * K + s] = -1;
 }
 
 // The backward's pointwise step (bwd_expand_kernel) from the 8-bit set, and x restored beside it.  A wavefront takes kAct8Span channels of

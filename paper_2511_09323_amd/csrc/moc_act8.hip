@@ -16,13 +16,18 @@ moc_status check_width(const moc_shape* shape) {
 
 template <class E> void save(const Dims& D, const E* x, const int32_t* idx, const E* g, const E* u, const moc_act8_set& set, hipStream_t st) {
     Span span("act8_save", st);
-    const size_t lds = (size_t)act8_blocks(D.F) * 4;
-    hipLaunchKernelGGL((act8_save_kernel<E>), dim3(D.T), dim3(256), lds, st, x, idx, g, u, D.d, D.F, D.K, set);
+    hipLaunchKernelGGL((act8_save_kernel<E>), dim3(D.T), dim3(256), (size_t)act8_blocks(D.F) * 4, st, x, idx, g, u, D.d, D.F, D.K, set);
 }
 
+// A wavefront a token has fewer to start and more to wait for in each, but takes longer for its token.  us, d 2048, F 5461, K 683, from memory: 2048 tokens 11.0 with one, 8.8
+// with four; 4096 14.2 and 15.7; 8192 27.1 and 32.7.
+constexpr int kAct8ManyTokens = 4096;
 template <class E> void load(const Dims& D, const moc_act8_set& set, E* x, int32_t* idx, E* g, E* u, hipStream_t st) {
     Span span("act8_load", st);
-    hipLaunchKernelGGL((act8_load_kernel<E>), dim3(D.T), dim3(256), 0, st, set, D.d, D.F, D.K, x, idx, g, u);
+    if (D.T < kAct8ManyTokens)
+        hipLaunchKernelGGL((act8_load_kernel<E, 4>), dim3(D.T), dim3(256), 0, st, set, D.T, D.d, D.F, D.K, x, idx, g, u);
+    else
+        hipLaunchKernelGGL((act8_load_kernel<E, 1>), dim3((unsigned)(((int64_t)D.T + 3) / 4)), dim3(256), 0, st, set, D.T, D.d, D.F, D.K, x, idx, g, u);
 }
 
 }  // namespace

@@ -69,6 +69,21 @@ def test_save_and_load(T, d, F, K, dtype):
     assert all(torch.equal(a, b) for a, b in zip(back, moc.moc_act8_load(saved, F, DT[dtype], out=out)))
 
 
+@pytest.mark.parametrize("T,d,F,K,dtype", [(5000, 136, 9000, 1100, "bf16"), (4097, 72, 171, 21, "f32"), (4099, 2056, 2048, 2048, "bf16")])
+def test_many_tokens(T, d, F, K, dtype):
+    """Tokens do not know of each other: all at once is a part after the other."""
+    x, idx, g, u = stored(T, d, F, K, dtype, T)
+    saved = moc.moc_act8_save(x, idx, g, u, F)
+    back = moc.moc_act8_load(saved, F, DT[dtype])
+    assert torch.equal(back[1], idx)
+    for r in (slice(0, 8), slice(1000, 3500), slice(T - 3, T)):
+        part = moc.moc_act8_save(*(t[r].clone() for t in (x, idx, g, u)), F)
+        assert all(torch.equal(a[r], b) for a, b in zip(saved, part))
+        assert all(torch.equal(a[r], b) for a, b in zip(back, moc.moc_act8_load(part, F, DT[dtype])))
+    r = slice(T - 3, T)
+    check_load(moc.Act8Set(*(t[r].clone() for t in saved)), F, dtype, [t[r] for t in back])
+
+
 def test_values_at_the_edges():
     """Zeros of both signs, blocks of subnormals and just above 2^-119, the largest values, values that round to 128, ties, infinities and NaN."""
     v = np.zeros((11, 64), dtype=np.float32)
