@@ -69,11 +69,13 @@ template <class E> __device__ __forceinline__ void act8_read(Act8Piece<E>& p, co
     if (left >= 8) {
         __builtin_memcpy(p.raw, v, sizeof(p.raw));
     } else {
+        float f[7] = {};
+        if (left > 0) {      // (no load in a branch of its own: each would be waited for before the next)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) p.set(k, 0.0f);
+            for (int k = 0; k < 7; ++k) f[k] = Elem<E>::load(v + min(k, left - 1));
+        }
 #pragma unroll
-        for (int k = 0; k < 7; ++k)
-            if (k < left) p.set(k, Elem<E>::load(v + k));
+        for (int k = 0; k < 8; ++k) p.set(k, k < 7 && k < left ? f[k % 7] : 0.0f);
     }
 }
 template <class E> __device__ __forceinline__ void act8_write(const Act8Piece<E>& p, E* v, int left) {
@@ -113,10 +115,12 @@ __device__ __forceinline__ u32x2_t act8_read_bytes(const int8_t* q, int left) {
     u32x2_t w{0, 0};
     if (left >= 8) {
         __builtin_memcpy(&w, q, 8);
-    } else {
+    } else if (left > 0) {
+        uint32_t b[7];
 #pragma unroll
-        for (int k = 0; k < 7; ++k)
-            if (k < left) w[k / 4] |= (uint32_t)(uint8_t)q[k] << (k % 4 * 8);
+        for (int k = 0; k < 7; ++k) b[k] = (uint8_t)q[min(k, left - 1)];
+#pragma unroll
+        for (int k = 0; k < 7; ++k) w[k / 4] |= k < left ? b[k] << (k % 4 * 8) : 0u;
     }
     return w;
 }
