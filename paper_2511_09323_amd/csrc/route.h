@@ -73,8 +73,11 @@ template <class E, bool VEC> __device__ __forceinline__ void route_logits(const 
                 for (int i = 0; i < Vec16<E>::N; ++i) l[p + i] = -INFINITY;
         }
     } else {
+        // (every lane loads eight, the last one again and again past the end: a load in a branch of its own would be waited for before the next)
 #pragma unroll
-        for (int i = 0; i < kRoutePer; ++i) l[i] = e0 + i < experts ? Elem<E>::load(row + e0 + i) : -INFINITY;
+        for (int i = 0; i < kRoutePer; ++i) l[i] = Elem<E>::load(row + min(e0 + i, experts - 1));
+#pragma unroll
+        for (int i = 0; i < kRoutePer; ++i) l[i] = e0 + i < experts ? l[i] : -INFINITY;
     }
 }
 
@@ -449,12 +452,14 @@ __global__ __launch_bounds__(256) void route_bwd_kernel(int T, int experts, int 
         });
         const float scale = dloss ? dloss[0] : 0.0f;
         float c[kRoutePer];
+#pragma unroll
+        for (int i = 0; i < kRoutePer; ++i) c[i] = coef[min(e0 + i, experts - 1)];
         float all = 0.0f, part = 0.0f, wdw = 0.0f, pc = 0.0f;
 #pragma unroll
         for (int i = 0; i < kRoutePer; ++i) {
             const bool real = e0 + i < experts;
             ex[i] = real ? expf(l[i] - top) : 0.0f;
-            c[i] = real ? coef[e0 + i] : 0.0f;
+            c[i] = real ? c[i] : 0.0f;
             all += ex[i];
             part += chosen[i] ? ex[i] : 0.0f;
             wdw += chosen[i] ? ex[i] * dw[i] : 0.0f;
