@@ -305,7 +305,7 @@ __global__ __launch_bounds__(256) void act8_load_kernel(moc_act8_set set, int T,
 // assembled in LDS, zero everywhere else, and streamed out.  No wavefront waits for another.  The first `unpack_groups` workgroups restore x.
 // Rounded to E: dz', by the product that made it, and z', dg, du, which the matrix cores take in E; so the gradients are bit for bit those of
 // moc_ffn_bwd from the restored set (dz' in fp32 would add 90 MB to what that product and this launch each move at the first of the sizes below).
-// Bound by memory: 8192 x 5461, K 683, x 8192 x 2048: 430 MB in 84 us, 5.1 TB/s, the rate of a large copy; 16384 x 2048, K 384, x 16384 x 768: 306 MB in 72 us.
+// Bound by memory: 8192 x 5461, K 683, x 8192 x 2048: 430 MB in 84 us, 5.1 TB/s, the rate of a large copy; 16384 x 2048, K 384, x 16384 x 768: 325 MB in 70 us.
 constexpr int kAct8Span = 1024;
 template <class E>
 __global__ __launch_bounds__(256) void bwd_expand_act8_kernel(moc_act8_set set, const E* __restrict__ dzd, RowGroups groups, int rows, int T, int d, int F, int K, int64_t ldf,
@@ -366,30 +366,32 @@ __global__ __launch_bounds__(256) void bwd_expand_act8_kernel(moc_act8_set set, 
     const uint8_t *ge = set.ge + t * act8_blocks(K), *ue = set.ue + t * act8_blocks(K);
     const E* dzrow = dzd + t * ldf + c0;
 #pragma unroll
-    for (int q0 = 0; q0 < SLOTS; q0 += BATCH) {      // (what BATCH slots read is asked for before any is worked on)
+    for (int q0 = 0; q0 < SLOTS; q0 += BATCH) {
         if (q0 * 64 >= n) break;
-        float gv[BATCH], uv[BATCH], dz[BATCH];
+        // What BATCH slots read is asked for before any is worked on; lanes past the last slot read that one's, and nothing is converted yet: in a branch that
+        // would be waited for.
+        int gv[BATCH], uv[BATCH], ch[BATCH];
         uint32_t gx[BATCH], ux[BATCH];
+        E dz[BATCH];
 #pragma unroll
         for (int q = 0; q < BATCH; ++q) {
-            const int s = (q0 + q) * 64 + lane, block = (before + s) / kAct8Block;
-            if (s < n) {
-                gv[q] = (float)gq[s];
-                uv[q] = (float)uq[s];
-                gx[q] = ge[block];
-                ux[q] = ue[block];
-                dz[q] = Elem<E>::load(dzrow + channel[q0 + q]);
-            }
+            if ((q0 + q) * 64 >= n) break;
+            const int s = min((q0 + q) * 64 + lane, n - 1), block = (before + s) / kAct8Block;
+            ch[q] = (q0 + q) * 64 + lane < n ? channel[q0 + q] : 0;
+            gv[q] = gq[s];
+            uv[q] = uq[s];
+            gx[q] = ge[block];
+            ux[q] = ue[block];
+            dz[q] = dzrow[ch[q]];
         }
 #pragma unroll
         for (int q = 0; q < BATCH; ++q) {
             if ((q0 + q) * 64 + lane >= n) continue;
-            const int j = channel[q0 + q];
             float z, dg, du;
-            moc_bwd_pointwise(gv[q] * act8_step(gx[q]), uv[q] * act8_step(ux[q]), dz[q], z, dg, du);
-            Elem<E>::store(&span[wave][0][j], z);
-            Elem<E>::store(&span[wave][1][j], dg);
-            Elem<E>::store(&span[wave][2][j], du);
+            moc_bwd_pointwise((float)gv[q] * act8_step(gx[q]), (float)uv[q] * act8_step(ux[q]), Elem<E>::load(&dz[q]), z, dg, du);
+            Elem<E>::store(&span[wave][0][ch[q]], z);
+            Elem<E>::store(&span[wave][1][ch[q]], dg);
+            Elem<E>::store(&span[wave][2][ch[q]], du);
         }
     }
     ordered();
