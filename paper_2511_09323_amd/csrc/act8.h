@@ -35,8 +35,9 @@ template <int CTRL> __device__ __forceinline__ uint32_t dpp_max_u32(uint32_t v) 
 }
 __device__ __forceinline__ uint32_t quad_max_u32(uint32_t v) { return dpp_max_u32<0x4E>(dpp_max_u32<0xB1>(v)); }      // quad_perm [1,0,3,2], [2,3,0,1]
 
-// Rows are worked on in pieces of 8 values, 4 lanes a block.  Rows of K values start anywhere: pieces are loaded and stored at the element's alignment
-// (which the memory pipeline takes), the last ones of a row value by value.
+// Rows are worked on in pieces of 8 values, 4 lanes a block.  Rows of K values start anywhere: pieces are loaded and stored at the element's alignment, which the
+// memory pipeline takes at no measurable cost.  The last piece of a row, where it is not whole, is loaded as the row's last 8 values and shifted: loaded
+// value by value, the last pieces of the 1B layer's gate and up values took 4 us of the 29 that saving it took.
 template <class E> struct Act8Piece;
 template <> struct Act8Piece<float> {
     uint32_t raw[8];
@@ -48,6 +49,14 @@ template <> struct Act8Piece<float> {
     }
     __device__ __forceinline__ float value(int k) const { return __uint_as_float(raw[k]); }
     __device__ __forceinline__ void set(int k, float v) { raw[k] = __float_as_uint(v); }
+    __device__ __forceinline__ void shift(int by) {      // values `by` .. 7 to the front, zeros behind them (all zeros from 8 on)
+#pragma unroll
+        for (int o = 1; o < 8; o <<= 1)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) raw[k] = by & o ? (k + o < 8 ? raw[k + o & 7] : 0u) : raw[k];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) raw[k] = by >= 8 ? 0u : raw[k];
+    }
 };
 template <> struct Act8Piece<bf16_t> {
     uint32_t raw[4];
@@ -64,20 +73,44 @@ template <> struct Act8Piece<bf16_t> {
         const uint32_t b = __float_as_uint(v);
         raw[k / 2] = k & 1 ? (raw[k / 2] & 0xFFFFu) | (b & 0xFFFF0000u) : b >> 16;
     }
+    __device__ __forceinline__ void shift(int by) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) raw[k] = by & 1 ? __builtin_amdgcn_alignbit(k < 3 ? raw[k + 1 & 3] : 0u, raw[k], 16) : raw[k];
+#pragma unroll
+        for (int o = 1; o < 4; o <<= 1)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) raw[k] = by & 2 * o ? (k + o < 4 ? raw[k + o & 3] : 0u) : raw[k];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) raw[k] = by >= 8 ? 0u : raw[k];
+    }
 };
-template <class E> __device__ __forceinline__ void act8_read(Act8Piece<E>& p, const E* v, int left) {
-    if (left >= 8) {
-        __builtin_memcpy(p.raw, v, sizeof(p.raw));
+// The 8 values at value i of a row of n (n and the row the same in a wavefront): the load, and, apart from it, what makes the last ones of a row the lane's own.
+template <class E> __device__ __forceinline__ void act8_read(Act8Piece<E>& p, const E* row, int n, int i) {
+    if (n >= 8) {
+        __builtin_memcpy(p.raw, row + min(i, n - 8), sizeof(p.raw));
     } else {
-        float f[7] = {};
-        if (left > 0) {      // (no load in a branch of its own: each would be waited for before the next)
 #pragma unroll
-            for (int k = 0; k < 7; ++k) f[k] = Elem<E>::load(v + min(k, left - 1));
-        }
-#pragma unroll
-        for (int k = 0; k < 8; ++k) p.set(k, k < 7 && k < left ? f[k % 7] : 0.0f);
+        for (int k = 0; k < 8; ++k) p.set(k, i + k < n ? Elem<E>::load(row + i + k) : 0.0f);
     }
 }
+template <class E> __device__ __forceinline__ void act8_settle(Act8Piece<E>& p, int n, int i) {
+    if (n >= 8 && n - (i & ~511) < 512) p.shift(max(0, i - (n - 8)));      // (the wavefront's 512 values are not all there)
+}
+__device__ __forceinline__ uint64_t act8_read_bytes(const int8_t* row, int n, int i) {
+    uint64_t w = 0;
+    if (n >= 8) {
+        __builtin_memcpy(&w, row + min(i, n - 8), 8);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w |= i + k < n ? (uint64_t)(uint8_t)row[i + k] << (8 * k) : 0u;
+    }
+    return w;
+}
+__device__ __forceinline__ u32x2_t act8_settle_bytes(uint64_t w, int n, int i) {
+    if (n >= 8 && n - (i & ~511) < 512) w >>= 8 * min(7, max(0, i - (n - 8)));      // (nobody looks at values past the row's end)
+    return u32x2_t{(uint32_t)w, (uint32_t)(w >> 32)};
+}
+// The first `left` of 8 values, or all of them.
 template <class E> __device__ __forceinline__ void act8_write(const Act8Piece<E>& p, E* v, int left) {
     if (left >= 8) {
         __builtin_memcpy(v, p.raw, sizeof(p.raw));
@@ -85,6 +118,17 @@ template <class E> __device__ __forceinline__ void act8_write(const Act8Piece<E>
 #pragma unroll
         for (int k = 0; k < 7; ++k)
             if (k < left) Elem<E>::store(v + k, p.value(k));
+    }
+}
+__device__ __forceinline__ void act8_write_bytes(u32x2_t w, int8_t* q, int left) {
+    if (left >= 8) {
+        __builtin_memcpy(q, &w, 8);
+    } else if (left > 0) {
+        const uint32_t rest = left & 4 ? w[1] : w[0], last = left & 2 ? rest >> 16 : rest;
+        if (left & 4) __builtin_memcpy(q, &w, 4);
+        q += left & 4;
+        if (left & 2) __builtin_memcpy(q, &rest, 2);
+        if (left & 1) q[left & 2] = (int8_t)last;
     }
 }
 // Rounding: held to +-127 (which rounds to itself, so that it may come first), 1.5 2^23 added: the sum's last byte is the nearest whole number, halves to even,
@@ -111,29 +155,6 @@ template <class E> __device__ __forceinline__ void act8_unpack(u32x2_t w, uint32
 #pragma unroll
     for (int k = 0; k < 8; ++k) p.set(k, ((float)((w[k / 4] >> (k % 4 * 8)) & 0xFFu) - 128.0f) * step);
 }
-__device__ __forceinline__ u32x2_t act8_read_bytes(const int8_t* q, int left) {
-    u32x2_t w{0, 0};
-    if (left >= 8) {
-        __builtin_memcpy(&w, q, 8);
-    } else if (left > 0) {
-        uint32_t b[7];
-#pragma unroll
-        for (int k = 0; k < 7; ++k) b[k] = (uint8_t)q[min(k, left - 1)];
-#pragma unroll
-        for (int k = 0; k < 7; ++k) w[k / 4] |= k < left ? b[k] << (k % 4 * 8) : 0u;
-    }
-    return w;
-}
-__device__ __forceinline__ void act8_write_bytes(u32x2_t w, int8_t* q, int left) {
-    if (left >= 8) {
-        __builtin_memcpy(q, &w, 8);
-    } else {
-#pragma unroll
-        for (int k = 0; k < 7; ++k)
-            if (k < left) q[k] = (int8_t)(w[k / 4] >> (k % 4 * 8));
-    }
-}
-
 // A token's x, gate and up values in steps of 64 pieces, a piece a lane; a step lies in one of the three, so that all but a lane's offset stays in scalar registers.
 template <class V> struct Act8Step {
     V* v;
@@ -180,7 +201,7 @@ template <int WAVES> __device__ __forceinline__ void act8_sync() {
 
 // Saving, four wavefronts a token.  The steps are shared out over them and asked for together (8 steps, 1024 values of idx), so that a token of the usual sizes is one
 // trip to memory; then the mask, which is put together in LDS, and the pieces.  Entries of idx outside [0, F) are ignored.
-// 8192 tokens, d 2048, bf16: 24.9 us with K = 688 (4.6 TB/s of the 5.2 that a large copy reaches), 29.1 with K = 683, whose rows put the pieces at odd addresses.
+// 8192 tokens, d 2048, F 5461, K 683, bf16, from memory: 113 MB in 24.6 us, 4.6 TB/s of the 5.2 that a large copy reaches.
 constexpr int kAct8Steps = 8, kAct8Idx = 4;
 template <class E>
 __global__ __launch_bounds__(256) void act8_save_kernel(const E* __restrict__ x, const int32_t* __restrict__ idx, const E* __restrict__ g, const E* __restrict__ u, int d, int F,
@@ -202,7 +223,7 @@ __global__ __launch_bounds__(256) void act8_save_kernel(const E* __restrict__ x,
             const int s = s0 + i * 4 + wave;
             if (s >= steps) break;
             const Step at(s, set, t, d, K, x, g, u);
-            act8_read<E>(piece[i], at.v + at.piece(lane) * 8, at.left(lane));
+            act8_read<E>(piece[i], at.v, at.n, at.piece(lane) * 8);
         }
     };
     read(0);
@@ -224,6 +245,7 @@ __global__ __launch_bounds__(256) void act8_save_kernel(const E* __restrict__ x,
             if (s >= steps) break;
             const Step at(s, set, t, d, K, x, g, u);
             uint32_t e;
+            act8_settle<E>(piece[i], at.n, at.piece(lane) * 8);
             const u32x2_t w = act8_pack<E>(piece[i], e);
             act8_write_bytes(w, at.q + at.piece(lane) * 8, at.left(lane));
             if (at.in(lane) && (lane & 3) == 0) at.e[at.piece(lane) / 4] = (uint8_t)e;
@@ -233,7 +255,7 @@ __global__ __launch_bounds__(256) void act8_save_kernel(const E* __restrict__ x,
 
 // Restoring, shared out in the same way over one or four wavefronts a token, the channels first.  They go to LDS in the order of the set bits, 32 for each of the token's lanes at a time, and from there to
 // memory; a row with fewer than K bits (not one that was saved) leaves the rest of its indices at -1, bits past the K-th are dropped.
-// 8192 tokens, d 2048, F 5461, K 683, bf16: 113 MB in 27 us from memory (4.2 TB/s), in 21 where the set was just written.
+// 8192 tokens, d 2048, F 5461, K 683, bf16: 113 MB in 27.6 us from memory (4.1 TB/s), in 21 where the set was just written.
 template <class E, int WAVES>
 __global__ __launch_bounds__(256) void act8_load_kernel(moc_act8_set set, int T, int d, int F, int K, E* __restrict__ x, int32_t* __restrict__ idx, E* __restrict__ g,
                                                         E* __restrict__ u) {
@@ -251,7 +273,7 @@ __global__ __launch_bounds__(256) void act8_load_kernel(moc_act8_set set, int T,
     uint32_t head[WORDS];
 #pragma unroll
     for (int i = 0; i < WORDS; ++i) head[i] = i * LANES + tid < words ? sel[i * LANES + tid] : 0;
-    u32x2_t w[AHEAD];
+    uint64_t w[AHEAD];
     uint32_t e[AHEAD];
     const auto read = [&](int s0) {
 #pragma unroll
@@ -259,8 +281,8 @@ __global__ __launch_bounds__(256) void act8_load_kernel(moc_act8_set set, int T,
             const int s = s0 + i * WAVES + mine;
             if (s >= steps) break;
             const Step at(s, set, t, d, K, x, g, u);
-            w[i] = act8_read_bytes(at.q + at.piece(lane) * 8, at.left(lane));
-            e[i] = at.in(lane) ? at.e[at.piece(lane) / 4] : 0u;
+            w[i] = act8_read_bytes(at.q, at.n, at.piece(lane) * 8);
+            e[i] = at.e[min(at.piece(lane) / 4, act8_blocks(at.n) - 1)];
         }
     };
     read(0);
@@ -294,7 +316,7 @@ __global__ __launch_bounds__(256) void act8_load_kernel(moc_act8_set set, int T,
             if (s >= steps) break;
             const Step at(s, set, t, d, K, x, g, u);
             Act8Piece<E> piece;
-            act8_unpack<E>(w[i], e[i], piece);
+            act8_unpack<E>(act8_settle_bytes(w[i], at.n, at.piece(lane) * 8), e[i], piece);
             act8_write<E>(piece, at.v + at.piece(lane) * 8, at.left(lane));
         }
     }
@@ -318,7 +340,7 @@ __global__ __launch_bounds__(256) void bwd_expand_act8_kernel(moc_act8_set set, 
 #pragma unroll 4
             for (int i = (threadIdx.x & 63) * 8; i < d; i += 64 * 8) {
                 Act8Piece<E> piece;
-                act8_unpack<E>(act8_read_bytes(set.xq + t * d + i, d - i), set.xe[t * act8_blocks(d) + i / kAct8Block], piece);
+                act8_unpack<E>(act8_settle_bytes(act8_read_bytes(set.xq + t * d, d, i), d, i), set.xe[t * act8_blocks(d) + i / kAct8Block], piece);
                 act8_write<E>(piece, x + t * d + i, d - i);
             }
         return;

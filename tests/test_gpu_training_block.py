@@ -97,3 +97,36 @@ def test_training_step_of_a_block(dtype, padded):
         P.assert_close(n, n64(a), b, tol)
     if padded:
         assert not dlogits[-40:].any() and torch.equal(out[-40:], h[-40:])
+
+
+def test_two_graphs_share_a_workspace():
+    """Nothing in a workspace lasts from one call to the next: two captured steps of other sizes over one workspace, replayed in turn, are the eager ones."""
+    sizes = ((700, 640, 8, 2), (3000, 200, 64, 3))
+    need = max(max(moc.norm_bwd_workspace_bytes(T, d, torch.bfloat16), moc.route_workspace_bytes(T, E, k)) for T, d, E, k in sizes)
+    ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+    parts = []
+    for T, d, E, k in sizes:
+        h, dy, gain = (torch.randn(*s, device="cuda").bfloat16() for s in ((T, d), (T, d), (d,)))
+        logits = torch.randn(T, E, device="cuda")
+        grads = (torch.empty_like(h), torch.empty_like(gain), torch.empty_like(gain))
+        out = tuple(torch.empty_like(t) for t in moc.moc_route(logits, k))
+
+        def step(h=h, dy=dy, gain=gain, logits=logits, grads=grads, out=out, k=k):
+            moc.moc_layernorm_bwd(h, gain, EPS, dy, ws=ws, out=grads)
+            moc.moc_route(logits, k, ws=ws, out=out)
+        step()
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            step()
+        parts.append((g, step, grads + out, (h, dy, logits)))
+    for i in range(3):
+        for g, step, results, inputs in parts:
+            for t in inputs:
+                t.normal_()
+            g.replay()
+            torch.cuda.synchronize()
+            got = [t.clone() for t in results]
+            step()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(got, results)), i
