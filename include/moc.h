@@ -225,7 +225,7 @@ moc_status moc_rmsnorm(int32_t T, int32_t d, int32_t dtype, const void* h, const
 /* Backward of moc_rmsnorm.  With n = h / sqrt(mean(h^2) + eps) and p = dy . gain, a row of dh is
  * (p - n mean(p . n)) / sqrt(mean(h^2) + eps), plus dres's row if dres_or_null is not NULL (the gradient
  * that reaches h past the norm, over the residual connection); dgain[d] is the sum of dy . n over the
- * rows.  The statistics are computed again from h.  dh may be dy or dres.  Sums are fp32, in an order that
+ * rows.  eps may be 0; a row of zeros then is 0 / 0, as in moc_rmsnorm.  The statistics are computed again from h.  dh may be dy or dres.  Sums are fp32, in an order that
  * depends on T and d only; every output is rounded once.  d <= 16384 (MOC_ERR_UNSUPPORTED).  ws holds
  * moc_norm_bwd_workspace_bytes(T, d, dtype) bytes (0 if these are invalid). */
 moc_status moc_rmsnorm_bwd(int32_t T, int32_t d, int32_t dtype, const void* h, const void* gain, float eps,

@@ -215,6 +215,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_bwd_kernel(const E* __restr
         row.clean(in, ry);
         float mean, r;
         row_stats<E, FORM, NV, TPR, RMS>(row, rh, eps, sums, mean, r);
+        r = in ? r : 0.0f;      // (a slot without a row holds zeros, whose 1 / sqrt(0 + eps) is no number to multiply by where eps is 0; its n is 0 and adds nothing)
         float sp = 0.0f, spn = 0.0f;
 #pragma unroll
         for (int u = 0; u < NV; ++u) {
