@@ -326,7 +326,7 @@ __global__ __launch_bounds__(256) void act8_load_kernel(moc_act8_set set, int T,
 // one dense row: the mask bits give it its channels and, by the bits before them, their places in the compact rows; z', dg and du are
 // assembled in LDS, zero everywhere else, and streamed out.  No wavefront waits for another.  The first `unpack_groups` workgroups restore x.
 // Rounded to E: dz', by the product that made it, and z', dg, du, which the matrix cores take in E; so the gradients are bit for bit those of
-// moc_ffn_bwd from the restored set (dz' in fp32 would add 90 MB to what that product and this launch each move at the first of the sizes below).
+// moc_ffn_bwd from the restored set where it, too, takes this step in a launch of its own; where it does not, so does the backward from 8 bits (dz' in fp32 would add 90 MB to what that product and this launch each move at the first of the sizes below).
 // Bound by memory: 8192 x 5461, K 683, x 8192 x 2048: 430 MB in 84 us, 5.1 TB/s, the rate of a large copy; 16384 x 2048, K 384, x 16384 x 768: 325 MB in 70 us.
 constexpr int kAct8Span = 1024;
 template <class E>

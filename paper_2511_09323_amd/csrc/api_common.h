@@ -220,9 +220,29 @@ template <class E> struct BwdWs {      // dense [T, ldF] operands (+ the bit mas
     }
 };
 
-// The backward from an 8-bit set: x restored behind the other scratch.
-template <class E> E* act8_x(void* ws, const BwdWs<E>& W) { return reinterpret_cast<E*>(static_cast<unsigned char*>(ws) + W.bytes); }
-template <class E> size_t bwd_act8_bytes(const Dims& D) { return BwdWs<E>(nullptr, D, false).bytes + round_up_sz((size_t)D.T * D.d * sizeof(E), 256); }
+// The backward's pointwise step runs in a launch of its own, with three dense rows in LDS, or, of layers whose rows do not fit, in the product that makes dZ'.
+template <class E> size_t expand_lds_bytes(const Dims& D) { return (size_t)3 * D.ldF * sizeof(E); }
+template <class E> bool expand_fits(const Dims& D) { return expand_lds_bytes<E>(D) <= 160 * 1024 - 64; }
+template <class E> bool bwd_expands(const Dims& D) { return expand_fits<E>(D) && !options().bwd_epilogue; }
+
+// The backward from an 8-bit set: x restored behind the other scratch, and the rest of the set where the pointwise step is in the product.
+template <class E> struct Act8Ws {
+    E* x;
+    int32_t* idx = nullptr;
+    E *g = nullptr, *u = nullptr;
+    size_t bytes;
+    Act8Ws(void* ws, const Dims& D) {
+        Carver c(ws);
+        (void)c.take<unsigned char>(BwdWs<E>(nullptr, D, false).bytes);
+        x = c.take<E>((size_t)D.T * D.d);
+        if (!bwd_expands<E>(D)) {
+            idx = c.take<int32_t>((size_t)D.T * D.K);
+            g = c.take<E>((size_t)D.T * D.K);
+            u = c.take<E>((size_t)D.T * D.K);
+        }
+        bytes = c.off;
+    }
+};
 
 constexpr int kDecodeFusedMaxP = 512;
 
@@ -277,7 +297,7 @@ template <class E> size_t workspace_for(const Dims& D, int op) {
         case MOC_OP_SWIGLU_FWD: return FwdWs<E>(nullptr, D, true).bytes;
         case MOC_OP_SWIGLU_BWD: return BwdWs<E>(nullptr, D, true).bytes;
         case MOC_OP_FWD_KEYED: return FwdWs<E>(nullptr, D, false, true).bytes;
-        case MOC_OP_BWD_ACT8: return bwd_act8_bytes<E>(D);
+        case MOC_OP_BWD_ACT8: return Act8Ws<E>(nullptr, D).bytes;
     }
     return 0;
 }

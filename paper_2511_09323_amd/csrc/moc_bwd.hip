@@ -55,8 +55,7 @@ moc_status bwd_impl(const Dims& D, const E* x, const E* wg, const E* wu, const E
     moc_status s;
     const int Fs = round_up(D.F, 8);      // whole 16-byte pieces into the padded [T, ldF] array (its padding is never read)
     GemmProblem<E> pz{kc_operand<E>(dy, D.d), kc_operand<E>(wd, D.d), D.T, D.F, D.d, 0, false};
-    const size_t expand_lds = (size_t)3 * D.ldF * sizeof(E);
-    if (!DENSE && expand_lds <= 160 * 1024 - 64 && !options().bwd_epilogue) {
+    if (!DENSE && bwd_expands<E>(D)) {
         // dZ' = dD W_down^T (bp-1) stored densely, then the pointwise step (bp-2, bp-3) on the K stored
         // channels of every token, expanded to the dense-masked rows Z', dG, dU
         if ((s = run_gemm<E, false, false>("gemm_dz", pz, EpiStore<E>{W.dZd, D.ldF, Fs, 0}, st, &W.sk)) != MOC_OK) return s;
@@ -64,7 +63,7 @@ moc_status bwd_impl(const Dims& D, const E* x, const E* wg, const E* wu, const E
         LdsAttr<bwd_expand_kernel<E>, kMaxDynLds>::use();
         Span span("bwd_pointwise_expand", st);
         const int32_t off[2] = {0, D.T};
-        hipLaunchKernelGGL(kern, dim3(round_up(D.T, kRowPad)), dim3(256), expand_lds, st, idx, gvals, uvals, W.dZd, row_groups(1, off), D.K,
+        hipLaunchKernelGGL(kern, dim3(round_up(D.T, kRowPad)), dim3(256), expand_lds_bytes<E>(D), st, idx, gvals, uvals, W.dZd, row_groups(1, off), D.K,
                            D.F, (int64_t)D.ldF, W.Zd, W.dGd, W.dUd);
         HIP_TRY(hipGetLastError());
     } else {
@@ -151,8 +150,7 @@ moc_status bwd_experts_impl(const Dims& D, int n_exp, const int32_t* off, const 
                             const int32_t* idx, const E* gvals, const E* uvals, const E* dy, E* dx, E* dwg, E* dwu, E* dwd,
                             void* ws, hipStream_t st) {
     BwdWs<E> W(ws, D, false, false);
-    const size_t expand_lds = (size_t)3 * D.ldF * sizeof(E);
-    if (expand_lds > 160 * 1024 - 64) return fail(MOC_ERR_UNSUPPORTED, "F = %d too large for the expert backward", D.F);
+    if (!expand_fits<E>(D)) return fail(MOC_ERR_UNSUPPORTED, "F = %d too large for the expert backward", D.F);
     const RowGroups rg = row_groups(n_exp, off);      // the dense operands' rows (dz' and everything of the caller's: off)
     moc_status s;
     if ((s = bwd_experts_dz<E>(D, W, n_exp, off, wd, dy, st)) != MOC_OK) return s;
@@ -160,7 +158,7 @@ moc_status bwd_experts_impl(const Dims& D, int n_exp, const int32_t* off, const 
         auto kern = bwd_expand_kernel<E>;
         LdsAttr<bwd_expand_kernel<E>, kMaxDynLds>::use();
         Span span("bwd_pointwise_expand", st);
-        hipLaunchKernelGGL(kern, dim3(rg.row[n_exp]), dim3(256), expand_lds, st, idx, gvals, uvals, W.dZd, rg, D.K, D.F, (int64_t)D.ldF, W.Zd,
+        hipLaunchKernelGGL(kern, dim3(rg.row[n_exp]), dim3(256), expand_lds_bytes<E>(D), st, idx, gvals, uvals, W.dZd, rg, D.K, D.F, (int64_t)D.ldF, W.Zd,
                            W.dGd, W.dUd);
         HIP_TRY(hipGetLastError());
     }
@@ -181,23 +179,28 @@ template <class E> moc_status expand_act8(const Dims& D, BwdWs<E>& W, const moc_
 }
 
 template <class E>
-moc_status bwd_act8_impl(const Dims& D, const moc_act8_set& set, const E* wg, const E* wu, const E* wd, const E* dy, E* dx, E* dwg, E* dwu, E* dwd, void* ws, hipStream_t st) {
+moc_status bwd_act8_impl(const moc_shape* shape, const Dims& D, const moc_act8_set& set, const E* wg, const E* wu, const E* wd, const E* dy, E* dx, E* dwg, E* dwu, E* dwd,
+                         void* ws, hipStream_t st) {
+    const Act8Ws<E> A(ws, D);
+    moc_status s;
+    if (!bwd_expands<E>(D)) {      // (the product's epilogue takes dz' unrounded and the set as the forward left it)
+        if ((s = moc_act8_load(shape, &set, A.x, A.idx, A.g, A.u, st)) != MOC_OK) return s;
+        return bwd_impl<E, false>(D, A.x, wg, wu, wd, A.idx, A.g, A.u, dy, dx, dwg, dwu, dwd, ws, st);
+    }
     BwdWs<E> W(ws, D, false);
-    E* x = act8_x<E>(ws, W);
     const int Fs = round_up(D.F, 8);      // whole 16-byte pieces into the padded [T, ldF] array (its padding is never read)
     const GemmProblem<E> pz{kc_operand<E>(dy, D.d), kc_operand<E>(wd, D.d), D.T, D.F, D.d, 0, false};
     const int32_t off[2] = {0, D.T};
-    moc_status s;
     if ((s = run_gemm<E, false, false>("gemm_dz", pz, EpiStore<E>{W.dZd, D.ldF, Fs, 0}, st, &W.sk)) != MOC_OK) return s;
-    if ((s = expand_act8<E>(D, W, set, row_groups(1, off), x, st)) != MOC_OK) return s;
-    return bwd_products<E, false>(D, W, x, wg, wu, dy, dx, dwg, dwu, dwd, st);
+    if ((s = expand_act8<E>(D, W, set, row_groups(1, off), A.x, st)) != MOC_OK) return s;
+    return bwd_products<E, false>(D, W, A.x, wg, wu, dy, dx, dwg, dwu, dwd, st);
 }
 
 template <class E>
 moc_status bwd_experts_act8_impl(const Dims& D, int n_exp, const int32_t* off, const moc_act8_set& set, const E* wg, const E* wu, const E* wd, const E* dy, E* dx, E* dwg,
                                  E* dwu, E* dwd, void* ws, hipStream_t st) {
     BwdWs<E> W(ws, D, false, false);
-    E* x = act8_x<E>(ws, W);
+    E* x = Act8Ws<E>(ws, D).x;
     const RowGroups rg = row_groups(n_exp, off);
     moc_status s;
     if ((s = bwd_experts_dz<E>(D, W, n_exp, off, wd, dy, st)) != MOC_OK) return s;
@@ -286,9 +289,9 @@ moc_status moc_ffn_bwd_act8(const moc_shape* shape, const moc_act8_set* set, con
     MOC_SETUP();
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     if (shape->dtype == MOC_BF16)
-        return bwd_act8_impl<bf16_t>(D, *set, (const bf16_t*)wg, (const bf16_t*)wu, (const bf16_t*)wd, (const bf16_t*)dy, (bf16_t*)dx, (bf16_t*)dwg, (bf16_t*)dwu,
+        return bwd_act8_impl<bf16_t>(shape, D, *set, (const bf16_t*)wg, (const bf16_t*)wu, (const bf16_t*)wd, (const bf16_t*)dy, (bf16_t*)dx, (bf16_t*)dwg, (bf16_t*)dwu,
                                      (bf16_t*)dwd, ws, st);
-    return bwd_act8_impl<float>(D, *set, (const float*)wg, (const float*)wu, (const float*)wd, (const float*)dy, (float*)dx, (float*)dwg, (float*)dwu, (float*)dwd, ws, st);
+    return bwd_act8_impl<float>(shape, D, *set, (const float*)wg, (const float*)wu, (const float*)wd, (const float*)dy, (float*)dx, (float*)dwg, (float*)dwu, (float*)dwd, ws, st);
 }
 
 moc_status moc_ffn_bwd_experts_act8(const moc_shape* shape, int32_t n_experts, const int32_t* expert_offsets, const moc_act8_set* set, const void* wg, const void* wu,

@@ -1,0 +1,27 @@
+"""Host-side checks at the limits of the 8-bit sets, the norms and the router that need no GPU: sizes of workspaces and refusals before anything is launched."""
+import ctypes
+
+import pytest
+
+from paper_2511_09323_amd import binding as B
+
+FAKE = ctypes.c_void_p(0x1000)      # aligned, never dereferenced: validation fails first
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return B.load_library()
+
+
+def _set():
+    return ctypes.byref(B.MocAct8Set(*[0x1000] * 7))
+
+
+@pytest.mark.parametrize("dtype,size,last", [(B.MOC_BF16, 2, 27264), (B.MOC_F32, 4, 13632)])
+def test_workspaces_of_wide_layers_hold_the_whole_set(lib, dtype, size, last):
+    """Up to `last` channels the backward from 8 bits restores x alone, past it idx, gvals and uvals, too (every piece 256-byte aligned)."""
+    T, d, K = 40, 64, 300
+    for F in (last, last + 1):
+        shape = ctypes.byref(B.MocShape(T, d, F, K, dtype))
+        more = lib.moc_workspace_bytes(shape, B.OP_BWD_ACT8) - lib.moc_workspace_bytes(shape, B.OP_BWD)
+        assert 0 <= more - T * d * size - (T * K * (4 + 2 * size) if F > last else 0) < 4 * 256
