@@ -16,6 +16,11 @@ namespace moc {
 constexpr int kAct8Block = 32;
 inline __host__ __device__ int act8_blocks(int n) { return (n + kAct8Block - 1) / kAct8Block; }
 
+// The set from token t on.
+inline moc_act8_set act8_from(const moc_act8_set& s, int64_t t, int d, int F, int K) {
+    return moc_act8_set{s.xq + t * d, s.xe + t * act8_blocks(d), s.sel + t * act8_blocks(F), s.gq + t * K, s.ge + t * act8_blocks(K), s.uq + t * K, s.ue + t * act8_blocks(K)};
+}
+
 // The byte e of a block whose largest magnitude has these bits (an infinity or NaN anywhere gives at least 0x7F800000).
 __device__ __forceinline__ uint32_t act8_exponent(uint32_t amax_bits) {
     const uint32_t e = amax_bits >> 23;

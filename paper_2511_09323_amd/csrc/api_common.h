@@ -64,6 +64,12 @@ struct Span {
 // ------------------------------------------------------------------------ small helpers
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
+// A launch counts its work-items in 32 bits: f(first row, rows) for parts of at most 2^23 workgroups (of 256 threads) of T rows, one after the other.
+template <class F> void in_launches(int64_t T, int64_t rows_of_a_group, const F& f) {
+    const int64_t most = rows_of_a_group << 23;
+    for (int64_t t0 = 0; t0 < T; t0 += most) f(t0, (int)std::min(most, T - t0));
+}
+
 struct Carver {   // hands out 256-byte aligned pieces of the workspace
     unsigned char* base;
     size_t off = 0;

@@ -16,7 +16,10 @@ moc_status check_width(const moc_shape* shape) {
 
 template <class E> void save(const Dims& D, const E* x, const int32_t* idx, const E* g, const E* u, const moc_act8_set& set, hipStream_t st) {
     Span span("act8_save", st);
-    hipLaunchKernelGGL((act8_save_kernel<E>), dim3(D.T), dim3(256), (size_t)act8_blocks(D.F) * 4, st, x, idx, g, u, D.d, D.F, D.K, set);
+    in_launches(D.T, 1, [&](int64_t t, int n) {
+        hipLaunchKernelGGL((act8_save_kernel<E>), dim3(n), dim3(256), (size_t)act8_blocks(D.F) * 4, st, x + t * D.d, idx + t * D.K, g + t * D.K, u + t * D.K, D.d, D.F, D.K,
+                           act8_from(set, t, D.d, D.F, D.K));
+    });
 }
 
 // A wavefront a token has fewer to start and more to wait for in each, but takes longer for its token.  us, d 2048, F 5461, K 683, from memory: 2048 tokens 11.0 with one, 8.8
@@ -27,7 +30,10 @@ template <class E> void load(const Dims& D, const moc_act8_set& set, E* x, int32
     if (D.T < kAct8ManyTokens)
         hipLaunchKernelGGL((act8_load_kernel<E, 4>), dim3(D.T), dim3(256), 0, st, set, D.T, D.d, D.F, D.K, x, idx, g, u);
     else
-        hipLaunchKernelGGL((act8_load_kernel<E, 1>), dim3((unsigned)(((int64_t)D.T + 3) / 4)), dim3(256), 0, st, set, D.T, D.d, D.F, D.K, x, idx, g, u);
+        in_launches(D.T, 4, [&](int64_t t, int n) {
+            hipLaunchKernelGGL((act8_load_kernel<E, 1>), dim3((unsigned)(((int64_t)n + 3) / 4)), dim3(256), 0, st, act8_from(set, t, D.d, D.F, D.K), n, D.d, D.F, D.K, x + t * D.d,
+                               idx + t * D.K, g + t * D.K, u + t * D.K);
+        });
 }
 
 }  // namespace

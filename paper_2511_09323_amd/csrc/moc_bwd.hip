@@ -166,11 +166,19 @@ moc_status bwd_experts_impl(const Dims& D, int n_exp, const int32_t* off, const 
 }
 
 // ---------------------------------------------------------------- backward from the 8-bit set
+// Launches of a whole workgroup for a row, as moc_ffn_bwd's are, or for four spans of a row have fewer than 2^32 work-items: 2^24 workgroups, less those that
+// restore x and the zero rows behind every expert's.
+moc_status check_act8_rows(const moc_shape* shape) {
+    const int64_t groups = (int64_t)shape->T * ((shape->F + 4 * kAct8Span - 1) / (4 * kAct8Span));
+    if (groups > (1 << 24) - 8192) return fail(MOC_ERR_UNSUPPORTED, "T = %d rows of F = %d channels are too many for the backward from 8 bits", shape->T, shape->F);
+    return MOC_OK;
+}
+
 // The pointwise step from the set, and x restored, in one launch.
 template <class E> moc_status expand_act8(const Dims& D, BwdWs<E>& W, const moc_act8_set& set, const RowGroups& rg, E* x, hipStream_t st) {
     Span span("bwd_pointwise_act8", st);
     const int rows = rg.row[rg.n];
-    const int64_t tasks = (int64_t)rows * ((D.ldF + kAct8Span - 1) / kAct8Span), groups = (tasks + 3) / 4;      // (T F < 2^40: tasks < 2^32)
+    const int64_t tasks = (int64_t)rows * ((D.ldF + kAct8Span - 1) / kAct8Span), groups = (tasks + 3) / 4;      // (fewer than 2^24 with those that restore x: check_act8_rows)
     const int unpack = std::min((D.T + 3) / 4, 2048);
     hipLaunchKernelGGL((bwd_expand_act8_kernel<E>), dim3((unsigned)(unpack + groups)), dim3(256), 0, st, set, W.dZd, rg, rows, D.T, D.d, D.F, D.K,
                        (int64_t)D.ldF, unpack, x, W.Zd, W.dGd, W.dUd);
@@ -282,7 +290,7 @@ moc_status moc_ffn_bwd_act8(const moc_shape* shape, const moc_act8_set* set, con
                             void* dwu, void* dwd, void* ws, size_t ws_bytes, void* hip_stream) {
     moc_status s = check_shape(shape, false);
     if (s != MOC_OK) return s;
-    if ((s = check_act8_set(set)) != MOC_OK) return s;
+    if ((s = check_act8_rows(shape)) != MOC_OK || (s = check_act8_set(set)) != MOC_OK) return s;
     CHECK_PTR(wg); CHECK_PTR(wu); CHECK_PTR(wd); CHECK_PTR(dy); CHECK_PTR(dx); CHECK_PTR(dwg); CHECK_PTR(dwu); CHECK_PTR(dwd);
     CHECK_WS(MOC_OP_BWD_ACT8);
     Dims D(*shape);
@@ -299,7 +307,7 @@ moc_status moc_ffn_bwd_experts_act8(const moc_shape* shape, int32_t n_experts, c
     moc_status s = check_shape(shape, false);
     if (s != MOC_OK) return s;
     if ((s = check_offsets(shape, n_experts, expert_offsets)) != MOC_OK) return s;
-    if ((s = check_act8_set(set)) != MOC_OK) return s;
+    if ((s = check_act8_rows(shape)) != MOC_OK || (s = check_act8_set(set)) != MOC_OK) return s;
     CHECK_PTR(wg); CHECK_PTR(wu); CHECK_PTR(wd); CHECK_PTR(dy); CHECK_PTR(dx); CHECK_PTR(dwg); CHECK_PTR(dwu); CHECK_PTR(dwd);
     CHECK_WS(MOC_OP_BWD_ACT8);
     Dims D(*shape);

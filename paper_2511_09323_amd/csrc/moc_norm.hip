@@ -56,7 +56,10 @@ template <class E> moc_status layernorm(int T, int d, const E* h, const E* gain,
     Span span("layernorm", st);
     for_row<E, 16 / Vec16<E>::N, 64, 64, 256>(d, T < 1024 ? 256 : 64, [&](auto form, auto NV, auto TPR) {
         constexpr int rows = 256 / TPR;
-        hipLaunchKernelGGL((layernorm_kernel<E, decltype(form)::value, NV, TPR>), dim3((unsigned)(((int64_t)T + rows - 1) / rows)), dim3(256), 0, st, h, gain, bias, eps, T, d, out);
+        in_launches(T, rows, [&](int64_t t0, int n) {
+            hipLaunchKernelGGL((layernorm_kernel<E, decltype(form)::value, NV, TPR>), dim3((unsigned)(((int64_t)n + rows - 1) / rows)), dim3(256), 0, st, h + t0 * d, gain, bias, eps,
+                               n, d, out + t0 * d);
+        });
     });
     HIP_TRY(hipGetLastError());
     return MOC_OK;

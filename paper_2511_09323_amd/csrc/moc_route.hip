@@ -69,8 +69,10 @@ moc_status route_bwd(int T, int experts, int k, bool renorm, const E* logits, co
     Span span("route_bwd", st);
     for_token<E>(experts, [&](auto L, auto vec) {
         constexpr int tokens = 256 / L;
-        hipLaunchKernelGGL((route_bwd_kernel<E, L, vec>), dim3((T + tokens - 1) / tokens), dim3(256), 0, st, T, experts, k, renorm, logits, ids, coef, dweights, dloss,
-                           dlogits);
+        in_launches(T, tokens, [&](int64_t t0, int n) {
+            hipLaunchKernelGGL((route_bwd_kernel<E, L, vec>), dim3((n + tokens - 1) / tokens), dim3(256), 0, st, n, experts, k, renorm, logits + t0 * experts, ids + t0 * k, coef,
+                               dweights ? dweights + t0 * k : nullptr, dloss, dlogits + t0 * experts);
+        });
     });
     HIP_TRY(hipGetLastError());
     return MOC_OK;

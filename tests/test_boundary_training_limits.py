@@ -25,3 +25,13 @@ def test_workspaces_of_wide_layers_hold_the_whole_set(lib, dtype, size, last):
         shape = ctypes.byref(B.MocShape(T, d, F, K, dtype))
         more = lib.moc_workspace_bytes(shape, B.OP_BWD_ACT8) - lib.moc_workspace_bytes(shape, B.OP_BWD)
         assert 0 <= more - T * d * size - (T * K * (4 + 2 * size) if F > last else 0) < 4 * 256
+
+
+def test_rows_past_a_launch_are_refused_by_the_backward_from_8_bits(lib):
+    """Before anything is launched: -3, and what the next check finds (a workspace too small) up to the limit."""
+    most = (1 << 24) - 8192
+    for T, F, rc in ((most, 4096, -2), (most + 1, 4096, -3), (most // 2, 4097, -2), (most // 2 + 1, 4097, -3), (most // 2, 8192, -2), (most // 2, 8193, -3), (1 << 24, 32, -3),
+                     (2147483647, 64, -3)):
+        shape = ctypes.byref(B.MocShape(T, 8, F, 1, B.MOC_BF16))
+        assert lib.moc_ffn_bwd_act8(shape, _set(), *[FAKE] * 9, 256, None) == rc, (T, F)
+        assert lib.moc_ffn_bwd_experts_act8(shape, 1, (ctypes.c_int32 * 2)(0, T), _set(), *[FAKE] * 9, 256, None) == rc, (T, F)
