@@ -275,7 +275,7 @@ moc_status moc_act8_load(const moc_shape* shape, const moc_act8_set* set, void* 
  * moc_act8_load restores (for every F of theirs; the experts' limit on F does not hold here), without the restored
  * set in memory but for x, which the workspace (MOC_OP_BWD_ACT8) has room for.  Of layers whose pointwise step moc_ffn_bwd
  * takes inside a product (F > 27264 in bf16, 13632 in fp32) it holds idx, gvals and uvals, too.
- * T ceil(F / 4096) <= 2^24 - 8192 (MOC_ERR_UNSUPPORTED). */
+ * d <= 2^24 and T ceil(F / 4096) <= 2^24 - 8192 (MOC_ERR_UNSUPPORTED). */
 moc_status moc_ffn_bwd_act8(const moc_shape* shape, const moc_act8_set* set, const void* wg, const void* wu, const void* wd,
                             const void* dy, void* dx, void* dwg, void* dwu, void* dwd,
                             void* ws, size_t ws_bytes, void* hip_stream);

@@ -112,7 +112,7 @@ int device_cu_count();          // compute units of the current device (after en
 moc_status check_shape(const moc_shape* s, bool decode);
 moc_status check_group(int F, int K, int ga, int gb);
 moc_status check_key_mode(int32_t key_mode);
-moc_status check_act8_set(const moc_act8_set* set);
+moc_status check_act8_set(const moc_shape* shape, const moc_act8_set* set);
 moc_status check_offsets(const moc_shape* shape, int32_t n_experts, const int32_t* off);
 
 #define CHECK_PTR(p)                                                                   \

@@ -8,12 +8,6 @@ using namespace mocapi;
 
 namespace {
 
-// (a step's offsets in a row stay in 32 bits)
-moc_status check_width(const moc_shape* shape) {
-    if (shape->d > 1 << 24) return fail(MOC_ERR_UNSUPPORTED, "d = %d exceeds 2^24", shape->d);
-    return MOC_OK;
-}
-
 template <class E> void save(const Dims& D, const E* x, const int32_t* idx, const E* g, const E* u, const moc_act8_set& set, hipStream_t st) {
     Span span("act8_save", st);
     in_launches(D.T, 1, [&](int64_t t, int n) {
@@ -43,7 +37,7 @@ extern "C" {
 moc_status moc_act8_save(const moc_shape* shape, const void* x, const int32_t* idx, const void* gvals, const void* uvals, const moc_act8_set* set, void* hip_stream) {
     moc_status s = check_shape(shape, false);
     if (s != MOC_OK) return s;
-    if ((s = check_width(shape)) != MOC_OK || (s = check_act8_set(set)) != MOC_OK) return s;
+    if ((s = check_act8_set(shape, set)) != MOC_OK) return s;
     CHECK_PTR(x); CHECK_PTR(idx); CHECK_PTR(gvals); CHECK_PTR(uvals);
     Dims D(*shape);
     MOC_SETUP();
@@ -57,7 +51,7 @@ moc_status moc_act8_save(const moc_shape* shape, const void* x, const int32_t* i
 moc_status moc_act8_load(const moc_shape* shape, const moc_act8_set* set, void* x, int32_t* idx, void* gvals, void* uvals, void* hip_stream) {
     moc_status s = check_shape(shape, false);
     if (s != MOC_OK) return s;
-    if ((s = check_width(shape)) != MOC_OK || (s = check_act8_set(set)) != MOC_OK) return s;
+    if ((s = check_act8_set(shape, set)) != MOC_OK) return s;
     CHECK_PTR(x); CHECK_PTR(idx); CHECK_PTR(gvals); CHECK_PTR(uvals);
     Dims D(*shape);
     MOC_SETUP();

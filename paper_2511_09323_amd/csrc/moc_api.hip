@@ -147,7 +147,9 @@ moc_status check_key_mode(int32_t key_mode) {
     return MOC_OK;
 }
 
-moc_status check_act8_set(const moc_act8_set* set) {
+moc_status check_act8_set(const moc_shape* shape, const moc_act8_set* set) {
+    // (offsets in a row stay in 32 bits)
+    if (shape->d > 1 << 24) return fail(MOC_ERR_UNSUPPORTED, "d = %d exceeds 2^24", shape->d);
     if (!set) return fail(MOC_ERR_BAD_ARG, "set is NULL");
     CHECK_PTR(set->xq); CHECK_PTR(set->xe); CHECK_PTR(set->sel); CHECK_PTR(set->gq); CHECK_PTR(set->ge); CHECK_PTR(set->uq); CHECK_PTR(set->ue);
     return MOC_OK;

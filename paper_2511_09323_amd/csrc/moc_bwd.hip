@@ -290,7 +290,7 @@ moc_status moc_ffn_bwd_act8(const moc_shape* shape, const moc_act8_set* set, con
                             void* dwu, void* dwd, void* ws, size_t ws_bytes, void* hip_stream) {
     moc_status s = check_shape(shape, false);
     if (s != MOC_OK) return s;
-    if ((s = check_act8_rows(shape)) != MOC_OK || (s = check_act8_set(set)) != MOC_OK) return s;
+    if ((s = check_act8_rows(shape)) != MOC_OK || (s = check_act8_set(shape, set)) != MOC_OK) return s;
     CHECK_PTR(wg); CHECK_PTR(wu); CHECK_PTR(wd); CHECK_PTR(dy); CHECK_PTR(dx); CHECK_PTR(dwg); CHECK_PTR(dwu); CHECK_PTR(dwd);
     CHECK_WS(MOC_OP_BWD_ACT8);
     Dims D(*shape);
@@ -307,7 +307,7 @@ moc_status moc_ffn_bwd_experts_act8(const moc_shape* shape, int32_t n_experts, c
     moc_status s = check_shape(shape, false);
     if (s != MOC_OK) return s;
     if ((s = check_offsets(shape, n_experts, expert_offsets)) != MOC_OK) return s;
-    if ((s = check_act8_rows(shape)) != MOC_OK || (s = check_act8_set(set)) != MOC_OK) return s;
+    if ((s = check_act8_rows(shape)) != MOC_OK || (s = check_act8_set(shape, set)) != MOC_OK) return s;
     CHECK_PTR(wg); CHECK_PTR(wu); CHECK_PTR(wd); CHECK_PTR(dy); CHECK_PTR(dx); CHECK_PTR(dwg); CHECK_PTR(dwu); CHECK_PTR(dwd);
     CHECK_WS(MOC_OP_BWD_ACT8);
     Dims D(*shape);

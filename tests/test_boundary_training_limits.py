@@ -35,3 +35,13 @@ def test_rows_past_a_launch_are_refused_by_the_backward_from_8_bits(lib):
         shape = ctypes.byref(B.MocShape(T, 8, F, 1, B.MOC_BF16))
         assert lib.moc_ffn_bwd_act8(shape, _set(), *[FAKE] * 9, 256, None) == rc, (T, F)
         assert lib.moc_ffn_bwd_experts_act8(shape, 1, (ctypes.c_int32 * 2)(0, T), _set(), *[FAKE] * 9, 256, None) == rc, (T, F)
+
+
+def test_widths_that_no_set_has_are_refused_by_all(lib):
+    for d, rc in (((1 << 24) + 8, -3), ((1 << 31) - 8, -3)):
+        shape, w = ctypes.byref(B.MocShape(1, d, 64, 8, B.MOC_BF16)), [FAKE] * 4
+        assert lib.moc_act8_save(shape, *w, _set(), None) == rc and lib.moc_act8_load(shape, _set(), *w, None) == rc
+        assert lib.moc_ffn_bwd_act8(shape, _set(), *[FAKE] * 9, 256, None) == rc
+        assert lib.moc_ffn_bwd_experts_act8(shape, 1, (ctypes.c_int32 * 2)(0, 1), _set(), *[FAKE] * 9, 256, None) == rc
+    shape = ctypes.byref(B.MocShape(1, 1 << 24, 64, 8, B.MOC_BF16))
+    assert lib.moc_ffn_bwd_act8(shape, _set(), *[FAKE] * 9, 256, None) == -2
