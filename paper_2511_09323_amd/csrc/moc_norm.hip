@@ -19,11 +19,12 @@ moc_status check_norm(int32_t T, int32_t d, int32_t dtype) {
 
 template <RowForm F> struct Form { static constexpr RowForm value = F; };
 
-// f(form of the rows, pieces of a lane, lanes of a row) for the fewest lanes, MIN .. MAX and at least `least`, that hold d
+// f(form of the rows, pieces of a lane, lanes of a row) for the fewest lanes, MIN .. MAX and at least `least` (MORE: may be more than d needs), that hold d
 // elements in NV pieces each (fewer than FULL lanes: NV / 2); rows that fill a half or a quarter of that take NV / 2 or NV / 4, rows past MAX lanes 2 or 4
 // times as many.
-template <class E, int NV, int FULL, int MIN, int MAX, class F> void for_row(int d, int least, const F& f) {
+template <class E, int NV, int FULL, int MIN, int MAX, bool MORE, class F> void for_row(int d, int least, const F& f) {
     constexpr int W = Vec16<E>::N, EL = NV * W;
+    constexpr bool PARTS = NV >= 4 && (MORE || MIN == 64);
     const auto with = [&](auto nv) {
         const std::integral_constant<int, MIN> lanes{};
         if (d % W == 0) f(Form<RowForm::Whole>{}, nv, lanes);
@@ -33,14 +34,14 @@ template <class E, int NV, int FULL, int MIN, int MAX, class F> void for_row(int
         if (d < W) return f(Form<RowForm::Narrow>{}, std::integral_constant<int, 1>{}, std::integral_constant<int, 64>{});
     }
     if constexpr (MIN < MAX) {
-        if (MIN < least || d > MIN * (MIN < FULL ? EL / 2 : EL)) return for_row<E, NV, FULL, 2 * MIN, MAX>(d, least, f);
-        if constexpr (NV >= 4) {
+        if (MIN < least || d > MIN * (MIN < FULL ? EL / 2 : EL)) return for_row<E, NV, FULL, 2 * MIN, MAX, MORE>(d, least, f);
+        if constexpr (PARTS) {
             if (d <= MIN * EL / 4) return with(std::integral_constant<int, NV / 4>{});
             if (d <= MIN * EL / 2) return with(std::integral_constant<int, NV / 2>{});
         }
         if constexpr (MIN >= FULL) with(std::integral_constant<int, NV>{});
     } else {
-        if constexpr (NV >= 4) {
+        if constexpr (PARTS) {
             if (d <= MIN * EL / 4) return with(std::integral_constant<int, NV / 4>{});
             if (d <= MIN * EL / 2) return with(std::integral_constant<int, NV / 2>{});
         }
@@ -54,7 +55,9 @@ template <class E, int NV, int FULL, int MIN, int MAX, class F> void for_row(int
 
 template <class E> moc_status layernorm(int T, int d, const E* h, const E* gain, const E* bias, float eps, E* out, hipStream_t st) {
     Span span("layernorm", st);
-    for_row<E, 16 / Vec16<E>::N, 64, 64, 256>(d, T < 1024 ? 256 : 64, [&](auto form, auto NV, auto TPR) {
+    // The fewest lanes that hold a row, however many rows there are: a row's bits do not depend on the others, and 256 lanes for few rows gain little or lose.  us with the fewest
+    // and with 256: bf16 1 x 512 1.70 and 1.93, 512 x 1024 2.05 and 2.77, 128 x 2048 2.24 and 2.26; fp32 512 x 768 2.57 and 2.72, 128 x 2048 2.40 and 2.24.
+    for_row<E, 16 / Vec16<E>::N, 64, 64, 256, false>(d, 64, [&](auto form, auto NV, auto TPR) {
         constexpr int rows = 256 / TPR;
         in_launches(T, rows, [&](int64_t t0, int n) {
             hipLaunchKernelGGL((layernorm_kernel<E, decltype(form)::value, NV, TPR>), dim3((unsigned)(((int64_t)n + rows - 1) / rows)), dim3(256), 0, st, h + t0 * d, gain, bias, eps,
@@ -75,9 +78,9 @@ moc_status norm_bwd(int T, int d, const E* h, const E* gain, float eps, const E*
         // A few rows for more than one workgroup leave most of the chip idle, and what counts is how long a row takes: then a piece a lane.  bf16, us: 16 x 4096
         // 13.2 against 9.9, 128 x 2048 9.5 against 8.3; 512 x 4096 15.7 against 16.6; 4 x 2048, one workgroup otherwise, 6.3 against 7.6.
         int least = 64, rows_at_once = 0;
-        for_row<E, NV, FULL, 64, MAX>(d, least, [&](auto, auto, auto TPR) { rows_at_once = kNormThreads / TPR; });
+        for_row<E, NV, FULL, 64, MAX, true>(d, least, [&](auto, auto, auto TPR) { rows_at_once = kNormThreads / TPR; });
         while (T > rows_at_once && T <= kFewRows && least < MAX && least * Vec16<E>::N < d) least *= 2;
-        for_row<E, NV, FULL, 64, MAX>(d, least, [&](auto form, auto NV, auto TPR) {
+        for_row<E, NV, FULL, 64, MAX, true>(d, least, [&](auto form, auto NV, auto TPR) {
             constexpr int rows = kNormThreads / TPR;
             groups = (int)std::min<int64_t>(kNormGroups, ((int64_t)T + rows - 1) / rows);
             hipLaunchKernelGGL((norm_bwd_kernel<E, decltype(form)::value, NV, TPR, RMS, BIAS>), dim3(groups), dim3(kNormThreads), 0, st, h, gain, eps, dy, dres, T, d, dh, part, dgain, dbias);
