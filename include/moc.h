@@ -292,7 +292,8 @@ moc_status moc_ffn_bwd_experts_act8(const moc_shape* shape, int32_t n_experts, c
  * what moc_ffn_fwd_experts takes -- and -1 behind the last of them.  With A the sum of counts and N the
  * tokens that have a slot, loss[1] = E sum_e (counts_e / A) (sum_t p_te / N), p the softmax of those tokens, and
  * coef[E] = E counts_e / (A N), its derivative by any p_te (all zero if no token has a slot).  A NaN is never chosen either
- * and makes the loss NaN.  The same inputs give the same bits.  T*k < 2^31 - 65536.  ws: moc_route_workspace_bytes. */
+ * and makes the loss NaN, and without renorm the weights of its token; +inf is chosen like any largest value and makes
+ * the loss and its token's weights NaN.  The weights of other tokens and of empty slots stay numbers.  The same inputs give the same bits.  T*k < 2^31 - 65536.  ws: moc_route_workspace_bytes. */
 size_t moc_route_workspace_bytes(int32_t T, int32_t E, int32_t k);
 moc_status moc_route(int32_t T, int32_t E, int32_t k, int32_t dtype, int32_t renorm, const void* logits,
                      const uint8_t* valid_or_null, int32_t* ids, float* weights, int32_t* counts, int32_t* order,
@@ -300,7 +301,7 @@ moc_status moc_route(int32_t T, int32_t E, int32_t k, int32_t dtype, int32_t ren
 
 /* Gradient of the router: dlogits[T,E] (dtype) from ids and coef of moc_route, dweights[T,k] (fp32) and dloss[1] (fp32);
  * either may be NULL, for zero.  No gradient flows through the choice or the counts.  Rows of tokens without a slot
- * are zero.  dweights of empty slots is not read into any result.  dlogits may be logits. */
+ * are zero; rows with a NaN or +inf among the logits of a token that has a slot are NaN.  dweights of empty slots is not read into any result.  dlogits may be logits. */
 moc_status moc_route_bwd(int32_t T, int32_t E, int32_t k, int32_t dtype, int32_t renorm, const void* logits,
                          const int32_t* ids, const float* coef, const float* dweights_or_null,
                          const float* dloss_or_null, void* dlogits, void* hip_stream);

@@ -372,7 +372,7 @@ template <class E, int L, bool VEC, bool ONE> __global__ __launch_bounds__(route
             const int j = r * L + lane;
             if (j >= a.k) continue;
             a.ids[(int64_t)t * a.k + j] = mine_e[r];
-            a.weights[(int64_t)t * a.k + j] = mine_x[r] / by;
+            a.weights[(int64_t)t * a.k + j] = mine_e[r] < 0 ? 0.0f : mine_x[r] / by;      // (by may be NaN)
             if (mine_e[r] < 0) continue;
             atomicAdd(&hist[mine_e[r]], 1);
             if (ONE) atomicOr(&mask[mine_e[r] * 8 + (t >> 5)], 1u << (t & 31));
