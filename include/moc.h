@@ -86,7 +86,7 @@ typedef enum {
     MOC_OP_SWIGLU_FWD = 3,
     MOC_OP_SWIGLU_BWD = 4,
     MOC_OP_FWD_KEYED = 5,      /* moc_ffn_fwd_keyed: the forward workspace plus one fp32 [T, F] key array */
-    MOC_OP_BWD_ACT8 = 6        /* moc_ffn_bwd_act8, moc_ffn_bwd_experts_act8: the backward workspace plus x, restored */
+    MOC_OP_BWD_ACT8 = 6        /* moc_ffn_bwd_act8, moc_ffn_bwd_experts_act8: the backward workspace and what is restored there */
 } moc_op;
 
 /* What the row Top-K ranks (ablation "Effect of top-K's position" and the remark after the proof
@@ -275,7 +275,8 @@ moc_status moc_act8_load(const moc_shape* shape, const moc_act8_set* set, void* 
  * moc_act8_load restores (for every F of theirs; the experts' limit on F does not hold here), without the restored
  * set in memory but for x, which the workspace (MOC_OP_BWD_ACT8) has room for.  Of layers whose pointwise step moc_ffn_bwd
  * takes inside a product (F > 27264 in bf16, 13632 in fp32) it holds idx, gvals and uvals, too.
- * d <= 2^24 and T ceil(F / 4096) <= 2^24 - 8192 (MOC_ERR_UNSUPPORTED). */
+ * bf16 values between the products are rounded where moc_ffn_bwd rounds them: dZ' as its product stores it, Z', dG and
+ * dU as the next products take them.  d <= 2^24 and T ceil(F / 4096) <= 2^24 - 8192 (MOC_ERR_UNSUPPORTED). */
 moc_status moc_ffn_bwd_act8(const moc_shape* shape, const moc_act8_set* set, const void* wg, const void* wu, const void* wd,
                             const void* dy, void* dx, void* dwg, void* dwu, void* dwd,
                             void* ws, size_t ws_bytes, void* hip_stream);
@@ -288,12 +289,14 @@ moc_status moc_ffn_bwd_experts_act8(const moc_shape* shape, int32_t n_experts, c
  * ids[T,k], and weights[T,k] (fp32), the softmax of the row there, divided by their sum if renorm is not 0.  A logit of -inf
  * is never chosen: slots that find nothing else hold -1 and weight 0.  A token whose byte in valid_or_null is 0
  * (padding) has no slots, whatever its logits are.  counts[E] are the experts' slots; order[T*k] lists the
- * slots, t*k + j, by expert and for each expert by token -- rows of x in this order and the running sum of counts are
- * what moc_ffn_fwd_experts takes -- and -1 behind the last of them.  With A the sum of counts and N the
+ * slots, t*k + j, by expert and for each expert by token, and -1 behind the last of them.  Rows of x in this order and the
+ * running sum of counts are what moc_ffn_fwd_experts takes, for 8 experts at most; its offsets are HOST memory, so that its
+ * caller copies counts and waits for them.  With A the sum of counts and N the
  * tokens that have a slot, loss[1] = E sum_e (counts_e / A) (sum_t p_te / N), p the softmax of those tokens, and
  * coef[E] = E counts_e / (A N), its derivative by any p_te (all zero if no token has a slot).  A NaN is never chosen either
- * and makes the loss NaN, and without renorm the weights of its token; +inf is chosen like any largest value and makes
- * the loss and its token's weights NaN.  The weights of other tokens and of empty slots stay numbers.  The same inputs give the same bits.  T*k < 2^31 - 65536.  ws: moc_route_workspace_bytes. */
+ * and makes the loss NaN, and without renorm the weights of its token; +inf is chosen like any largest value and makes the
+ * loss and the weights of its token NaN.  Empty slots weigh 0 there, too, and no other token's weights change.  The same
+ * inputs give the same bits.  T*k < 2^31 - 65536.  ws: moc_route_workspace_bytes. */
 size_t moc_route_workspace_bytes(int32_t T, int32_t E, int32_t k);
 moc_status moc_route(int32_t T, int32_t E, int32_t k, int32_t dtype, int32_t renorm, const void* logits,
                      const uint8_t* valid_or_null, int32_t* ids, float* weights, int32_t* counts, int32_t* order,
@@ -301,7 +304,8 @@ moc_status moc_route(int32_t T, int32_t E, int32_t k, int32_t dtype, int32_t ren
 
 /* Gradient of the router: dlogits[T,E] (dtype) from ids and coef of moc_route, dweights[T,k] (fp32) and dloss[1] (fp32);
  * either may be NULL, for zero.  No gradient flows through the choice or the counts.  Rows of tokens without a slot
- * are zero; rows with a NaN or +inf among the logits of a token that has a slot are NaN.  dweights of empty slots is not read into any result.  dlogits may be logits. */
+ * are zero, those of a token that has one and a NaN or +inf among its logits are NaN.  dweights of empty slots is not
+ * read into any result.  dlogits may be logits. */
 moc_status moc_route_bwd(int32_t T, int32_t E, int32_t k, int32_t dtype, int32_t renorm, const void* logits,
                          const int32_t* ids, const float* coef, const float* dweights_or_null,
                          const float* dloss_or_null, void* dlogits, void* hip_stream);

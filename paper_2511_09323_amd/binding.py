@@ -863,7 +863,8 @@ Route = collections.namedtuple("Route", "ids weights counts order loss coef")
 
 def moc_route(logits, k, valid=None, renorm=True, ws=None, out=None):
     """Softmax router: the k experts of every row of logits [T,E], their weights, the experts' counts, the slots in expert order,
-    the balance loss and its derivative by a token's probabilities.  valid: uint8 [T], 0 for padding.  Returns a Route."""
+    the balance loss and its derivative by a token's probabilities.  valid: uint8 [T], 0 for padding.  Returns a Route.  The expert entry points
+    take their row offsets from the host: counts.tolist(), which waits for the router, and at most 8 experts."""
     if out is not None and ws is not None:
         status = _fast.route(logits, k, valid, renorm, *out, ws)
         if status != _NOT_TAKEN:

@@ -188,7 +188,7 @@ template <class V> struct Act8Step {
 
 // Four or one wavefronts (WAVES) take a token.  Their number: a workgroup's four take four tokens, or one.  The eight chiplets, which take workgroups in turn, get an
 // eighth of the workgroups each, one behind the other: rows of K values and of block bytes end inside cache lines, and neighbours on one chiplet share its
-// cache, where on two they each move the line (the 1B layer's set restored in 26.4 us without, 23.6 with).
+// cache, where on two they each move the line (the 1B layer's set, just written, restored in 26.4 us without, 23.6 with, in the form that the kernel had then).
 template <int WAVES> __device__ __forceinline__ int64_t act8_token(int wave) {
     const unsigned chip = blockIdx.x & 7, each = gridDim.x >> 3, over = gridDim.x & 7;
     const int64_t group = (int64_t)chip * each + min(chip, over) + (blockIdx.x >> 3);
@@ -206,7 +206,8 @@ template <int WAVES> __device__ __forceinline__ void act8_sync() {
 
 // Saving, four wavefronts a token.  The steps are shared out over them and asked for together (8 steps, 1024 values of idx), so that a token of the usual sizes is one
 // trip to memory; then the mask, which is put together in LDS, and the pieces.  Entries of idx outside [0, F) are ignored.
-// 8192 tokens, d 2048, F 5461, K 683, bf16, from memory: 113 MB in 24.6 us, 4.6 TB/s of the 5.2 that a large copy reaches.
+// 8192 tokens, d 2048, F 5461, K 683, bf16: 113 MB from memory in 24.4 us, one such launch after the other (4.6 TB/s of the 5.2 that a large copy reaches); 27.5 in turn
+// with the restoring launch (4.1).
 constexpr int kAct8Steps = 8, kAct8Idx = 4;
 template <class E>
 __global__ __launch_bounds__(256) void act8_save_kernel(const E* __restrict__ x, const int32_t* __restrict__ idx, const E* __restrict__ g, const E* __restrict__ u, int d, int F,
@@ -260,7 +261,8 @@ __global__ __launch_bounds__(256) void act8_save_kernel(const E* __restrict__ x,
 
 // Restoring, shared out in the same way over one or four wavefronts a token, the channels first.  They go to LDS in the order of the set bits, 32 for each of the token's lanes at a time, and from there to
 // memory; a row with fewer than K bits (not one that was saved) leaves the rest of its indices at -1, bits past the K-th are dropped.
-// 8192 tokens, d 2048, F 5461, K 683, bf16: 113 MB in 27.6 us from memory (4.1 TB/s), in 21 where the set was just written.
+// 8192 tokens, d 2048, F 5461, K 683, bf16: 113 MB in 28 us from memory (4.0 TB/s), as in a backward pass long after its forward; in 21 where the set was just written
+// and is read from the last-level cache.
 template <class E, int WAVES>
 __global__ __launch_bounds__(256) void act8_load_kernel(moc_act8_set set, int T, int d, int F, int K, E* __restrict__ x, int32_t* __restrict__ idx, E* __restrict__ g,
                                                         E* __restrict__ u) {
@@ -332,7 +334,7 @@ __global__ __launch_bounds__(256) void act8_load_kernel(moc_act8_set set, int T,
 // assembled in LDS, zero everywhere else, and streamed out.  No wavefront waits for another.  The first `unpack_groups` workgroups restore x.
 // Rounded to E: dz', by the product that made it, and z', dg, du, which the matrix cores take in E; so the gradients are bit for bit those of
 // moc_ffn_bwd from the restored set where it, too, takes this step in a launch of its own; where it does not, so does the backward from 8 bits (dz' in fp32 would add 90 MB to what that product and this launch each move at the first of the sizes below).
-// Bound by memory: 8192 x 5461, K 683, x 8192 x 2048: 430 MB in 84 us, 5.1 TB/s, the rate of a large copy; 16384 x 2048, K 384, x 16384 x 768: 325 MB in 70 us.
+// Bound by memory: 8192 x 5461, K 683, x 8192 x 2048: 439 MB in 82 us, 5.3 TB/s, the rate of a large copy; 16384 x 2048, K 384, x 16384 x 768: 328 MB in 70 us.
 constexpr int kAct8Span = 1024;
 template <class E>
 __global__ __launch_bounds__(256) void bwd_expand_act8_kernel(moc_act8_set set, const E* __restrict__ dzd, RowGroups groups, int rows, int T, int d, int F, int K, int64_t ldf,

@@ -16,8 +16,10 @@ template <class E> void save(const Dims& D, const E* x, const int32_t* idx, cons
     });
 }
 
-// A wavefront a token has fewer to start and more to wait for in each, but takes longer for its token.  us, d 2048, F 5461, K 683, from memory: 2048 tokens 11.0 with one, 8.8
-// with four; 4096 14.2 and 15.7; 8192 27.1 and 32.7.
+// A wavefront a token has fewer to start and more to wait for in each, but takes longer for its token.  The line goes by the tokens alone: narrow layers would have it at
+// 2000, and of the largest sets, which memory bounds, four wavefronts take up to a tenth less.  bf16, sets from memory, us with one and with four: 512 x 1376, K 172,
+// 1024 tokens 4.4 and 4.0, 3000 5.9 and 7.1, 4096 7.2 and 9.2, 16384 17.7 and 28.6; 2048 x 5461, K 683, 2048 11.3 and 9.2, 4096 15.6 and 16.0, 6144 19.3 and 22.6, 16384 55.3
+// and 50.8; 4096 x 11008, K 1376, 2048 19.2 and 16.0, 4096 28.9 and 28.5, 6144 39.9 and 40.9, 16384 104 and 99.
 constexpr int kAct8ManyTokens = 4096;
 template <class E> void load(const Dims& D, const moc_act8_set& set, E* x, int32_t* idx, E* g, E* u, hipStream_t st) {
     Span span("act8_load", st);

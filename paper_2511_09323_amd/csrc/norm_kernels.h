@@ -126,7 +126,7 @@ __device__ __forceinline__ void row_stats(const Row<E, FORM, NV, TPR>& row, cons
     r = 1.0f / sqrtf(sums.sum<TPR>(ss) * scale + eps);
 }
 
-// One row per TPR lanes.  out may be h.  bf16, 8192 x 4096, from memory: 134 MB in 28.5 us, 4.7 TB/s (a large copy: 5.2).
+// One row per TPR lanes.  out may be h.  bf16, 8192 x 4096, from memory: 134 MB in 29 us, 4.6 TB/s (a large copy: 5.2).
 template <class E, RowForm FORM, int NV, int TPR>
 __global__ __launch_bounds__(256) void layernorm_kernel(const E* h, const E* __restrict__ gain, const E* __restrict__ bias, float eps, int T, int d, E* out) {
     constexpr int W = Vec16<E>::N;
@@ -159,7 +159,7 @@ __global__ __launch_bounds__(256) void layernorm_kernel(const E* h, const E* __r
 // dy up in registers.  (Loads come back in order, so nothing that is needed sooner is asked for after the next row: the gain is in LDS.)
 // A workgroup's sums are joined in LDS and written as one row of `part` ([workgroup][dgain, dbias][d]), or, where there is a single
 // workgroup, to dgain and dbias themselves.  dh may be dy or dres: an element is read by the lane that writes it, and where the lane beside it reads it too, it has
-// no use for it.  bf16, from memory: layer norm 8192 x 4096 201 MB in 39.5 us (5.1 TB/s), RMSNorm with dres 8192 x 2048 134 MB in 27 us (5.0 TB/s).
+// no use for it.  bf16, from memory: layer norm 8192 x 4096 201 MB in 40.5 us (5.0 TB/s), RMSNorm with dres 8192 x 2048 134 MB in 27 us (5.0 TB/s).
 constexpr int kNormThreads = 512;
 template <class E, RowForm FORM, int NV, int TPR, bool RMS, bool BIAS>
 __global__ __launch_bounds__(kNormThreads) void norm_bwd_kernel(const E* __restrict__ h, const E* __restrict__ gain, float eps, const E* dy, const E* dres, int T, int d, E* dh,

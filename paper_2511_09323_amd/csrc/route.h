@@ -11,8 +11,8 @@
 //
 // L lanes hold a token's logits, 8 each.  Routing is two launches (one, if a single workgroup does): slots and a histogram by
 // workgroup, then, with the histograms of the workgroups before it, every copy's place.  All are bound by launch and latency (a launch
-// that does nothing takes 1.3 us, one round trip to memory 1 to 2): us for slots, places, gradient: 37 tokens, 8 experts 4.4 in one, 2.8; 16384, 8 experts 4.2, 5.2,
-// 3.9; 32768, 64 experts, six slots 8.5, 6.5, 6.3 (8.4 MB of logits in and out).
+// that does nothing takes 1.3 us, one round trip to memory 1 to 2): us for slots, places, gradient: 37 tokens, 8 experts 4.5 in one, 2.9; 16384, 8 experts 4.4, 5.3,
+// 4.1; 32768, 64 experts, six slots 8.6, 6.4, 6.9 (8.4 MB of logits in and out).
 #pragma once
 #include "common.h"
 #include "misc_kernels.h"
